@@ -14,7 +14,8 @@
  * Conventions shared by every entry point
  * ---------------------------------------
  *  - All arrays are float32, row-major, contiguous, batch-major and live in
- *    device memory, except where an argument is marked "host".
+ *    device memory, except where an argument is marked "host" and where the layers at the
+ *    end (linear attention, layer normalisation) say otherwise.
  *  - x    [B, T+1, N]  observations x_0..x_T (N = forcing.n_forced).
  *  - z    [B, T, M]    states z_1..z_T; z[b, k] is z_{k+1}.
  *  - z0   [B, M]       initial state; NULL means z_0 = B^+ x_0 = [x_0; 0].
@@ -325,6 +326,105 @@ size_t deer_readout_workspace_bytes(const deer_readout *readout, int B, int T, i
 int deer_readout_loss(const deer_readout *readout, int B, int T, int M, const float *h, const float *x,
                       float *g, float *loss, uint32_t *masks, const deer_readout_grads *grads, void *ws,
                       size_t ws_bytes, void *stream);
+
+/* ---- linear attention with a decay for each head ------------------------------------
+ * The linear state-space layer whose state is a matrix S [Dk, Dv] for each of H heads:
+ *   S_t = a_t S_{t-1} + k_t v_t^T,   o_t = scale S_t^T q_t,   a_t = exp(log_decay_t).
+ * As for the diagonal SSM, deer_linattn computes every step of the sequence in parallel
+ * (chunks of steps as matrix products, the chunks joined by their decays), the adjoint is the
+ * same recurrence run backwards, and deer_linattn_step is the recurrence itself for one step
+ * (generation).  States, decays and every sum are float32 whatever the operands' type. */
+enum { DEER_F32 = 0, DEER_BF16 = 1, DEER_F16 = 2 };
+
+typedef struct {
+    int dtype;          /* DEER_F32, DEER_BF16 or DEER_F16: q, k, v, g, o and the gradients dq, dk, dv */
+    int H;              /* heads of v, o, log_decay and the state                             */
+    int Hk;             /* heads of q and k; H % Hk == 0, head h reads head h / (H / Hk)       */
+    int Dk, Dv;         /* 1..256 each                                                        */
+    int per_step;       /* log_decay: 0 for [H], 1 for [B, T, H] (a step: [B, H])             */
+    float scale;
+} deer_linattn_shape;
+
+/* An operand [B, T, heads, D] in device memory: element (b, t, h, d) at
+ * p + b sb + t st + h sh + d, strides >= 0 in elements (a slice of a fused projection is read
+ * in place; any alignment of the elements is allowed). */
+typedef struct {
+    const void *p;
+    int64_t sb, st, sh;
+} deer_view;
+
+/* Workspace bytes of deer_linattn (op = DEER_OP_SOLVE) and deer_linattn_adjoint
+ * (DEER_OP_ADJOINT).  Returns 0 for invalid arguments. */
+size_t deer_linattn_workspace_bytes(const deer_linattn_shape *shape, int B, int T, int op);
+
+/* The whole sequence.
+ *   log_decay  float32 [H] or [B, T, H] (per_step).  Values are meant to be <= 0; -inf is a
+ *              decay of zero: the state starts anew at that step (recordings laid end to end).
+ *              Positive values grow the state and are exact as long as the products of the
+ *              decays over any 64 steps and the states stay in float32's range.
+ *   lengths    int32 [B] or NULL (T): sequence b has lengths[b] steps (clamped to 0..T).  Rows
+ *              at and behind its end are not read; their outputs are zero.
+ *   state0     float32 [B, H, Dk, Dv] or NULL (zero): the state before the first step.
+ *   o          out [B, T, H, Dv] contiguous, of the operands' type, not an input's memory.
+ *   state      out float32 [B, H, Dk, Dv] or NULL: the state after each sequence's last step
+ *              (state0 for a length of 0).  May be state0 itself (a sequence continued in place).
+ * A NaN or an infinity among the rows that are read may reach any result of its sequence and
+ * head.  Fully asynchronous on `stream`; no two results depend on the order of atomics. */
+int deer_linattn(const deer_linattn_shape *shape, int B, int T, const deer_view *q, const deer_view *k,
+                 const deer_view *v, const float *log_decay, const int32_t *lengths, const float *state0, void *o,
+                 float *state, void *ws, size_t ws_bytes, void *stream);
+
+/* Its adjoint for the cotangents g = dL/do [B, T, H, Dv] and g_state = dL/dstate
+ * [B, H, Dk, Dv] (float32, NULL: zero):
+ *   R_t = a_{t+1} R_{t+1} + scale q_t g_t^T  (R = g_state behind the last step),
+ *   dq_t = scale S_t g_t,  dk_t = R_t v_t,  dv_t = R_t^T k_t,
+ *   dlog_decay_t = <R_t, a_t S_{t-1}>,  dstate0 = a_1 R_1  (g_state for a length of 0).
+ * dq, dk are sums over the heads that share them.  Outputs: dq, dk [B, T, Hk, Dk], dv
+ * [B, T, H, Dv] contiguous, of the operands' type, required, zero behind a sequence's end;
+ * dlog_decay float32 of log_decay's shape or NULL; dstate0 float32 [B, H, Dk, Dv] or NULL.
+ * The outputs may be no input's memory.  Fully asynchronous on `stream`. */
+int deer_linattn_adjoint(const deer_linattn_shape *shape, int B, int T, const deer_view *q, const deer_view *k,
+                         const deer_view *v, const float *log_decay, const int32_t *lengths, const float *state0,
+                         const deer_view *g, const float *g_state, void *dq, void *dk, void *dv, float *dlog_decay,
+                         float *dstate0, void *ws, size_t ws_bytes, void *stream);
+
+/* One step of every sequence: q, k [B, Hk, Dk], v [B, H, Dv] (views with st unused),
+ * log_decay [H] or [B, H] (per_step), state float32 [B, H, Dk, Dv] updated in place,
+ * o [B, H, Dv].  lengths int32 [B] or NULL: a sequence whose entry is <= 0 takes no step (its
+ * state stays as it is, its row of o is zero).  No workspace; fully asynchronous. */
+int deer_linattn_step(const deer_linattn_shape *shape, int B, const deer_view *q, const deer_view *k,
+                      const deer_view *v, const float *log_decay, const int32_t *lengths, float *state, void *o,
+                      void *stream);
+
+/* ---- layer normalisation ---------------------------------------------------------------
+ * Rows of D elements, each normalised by itself:
+ *   mean = sum x / D,  rstd = 1 / sqrt(sum (x - mean)^2 / D + eps),  y = (x - mean) rstd w + b,
+ * with weights for each of G groups: row i uses row i % G of w and b [G, D] (G = 1: the usual
+ * norm; x [B, T, H, D] and G = H: the norm of every head's output).  Statistics and sums are
+ * float32. */
+typedef struct {
+    int dtype;          /* DEER_F32, DEER_BF16 or DEER_F16: x, y, g, dx                        */
+    int wtype;          /* of w and b: DEER_F32 or dtype                                      */
+    int G, D;           /* D in 1..65536                                                      */
+    const void *w;      /* [G, D] or NULL (ones)                                              */
+    const void *b;      /* [G, D] or NULL (zeros)                                             */
+    float eps;          /* >= 0                                                               */
+} deer_norm;
+
+/* y [rows, D] (not x's memory), mean and rstd float32 [rows] or NULL.  rows a multiple of G.
+ * Fully asynchronous; no workspace. */
+int deer_layernorm(const deer_norm *norm, int64_t rows, const void *x, void *y, float *mean, float *rstd,
+                   void *stream);
+
+/* Its adjoint for the cotangent g = dL/dy, with the forward pass's mean and rstd: with
+ * xh = (x - mean) rstd and u = g w,
+ *   dx = rstd (u - mean(u) - xh mean(u xh)),   dw = sum over rows g xh,   db = sum over rows g.
+ * dx [rows, D] of x's type or NULL; dw, db float32 [G, D] or NULL.  The sums over the rows are
+ * taken in a fixed order.  Workspace: deer_layernorm_workspace_bytes(norm, rows).  The outputs
+ * may be no input's memory.  Fully asynchronous. */
+int deer_layernorm_adjoint(const deer_norm *norm, int64_t rows, const void *x, const void *g, const float *mean,
+                           const float *rstd, void *dx, float *dw, float *db, void *ws, size_t ws_bytes, void *stream);
+size_t deer_layernorm_workspace_bytes(const deer_norm *norm, int64_t rows);
 
 /* Residual and forced Jacobians of a PLRNN kind at trajectory z (eq. GTF_residual; the
  * Jacobian of F in the model-setup appendix; eq. error_forcing_decomp):

@@ -5,3 +5,4 @@ this package.  It shares no code with the HIP library.
 """
 from .deer_oracle import *  # noqa: F401,F403
 from . import brute  # noqa: F401
+from . import layers  # noqa: F401

@@ -9,6 +9,10 @@ Model dictionaries use the paper's names:
   shallow PLRNN  {"kind": "shplrnn", "A": [M], "W1": [M,L], "W2": [L,M], "h1": [M], "h2": [L]}
   diagonal SSM   {"kind": "diag_ssm", "lam": complex64 [M], "Bc": complex64 [M,K]}
   its read-out   {"Wa": [H,M], "ca": [H], "Wb": [No,H], "cb": [No]}
+
+The layers (deer_linattn, deer_linattn_adjoint, deer_linattn_step, deer_layernorm,
+deer_layernorm_adjoint) take GPU tensors in float32, bfloat16 or float16 as they are and run on
+the current stream of the tensors' GPU.
 """
 from __future__ import annotations
 
@@ -23,7 +27,8 @@ from ._binding import DeerError, load  # noqa: F401
 __all__ = ["deer_solve", "deer_adjoint", "deer_readout_loss", "plrnn_jacobian", "deer_scan", "deer_workspace_bytes",
            "deer_scan_workspace_bytes", "deer_readout_workspace_bytes", "deer_status_string", "DeerError", "load",
            "deer_sequential", "deer_sequential_workspace_bytes", "deer_solve_quasi", "deer_adjoint_quasi", "deer_train_step",
-           "deer_host_reserve"]
+           "deer_host_reserve", "deer_linattn", "deer_linattn_adjoint", "deer_linattn_step",
+           "deer_linattn_workspace_bytes", "deer_layernorm", "deer_layernorm_adjoint", "deer_layernorm_workspace_bytes"]
 
 _KINDS = {"plrnn": _b.DEER_PLRNN, "shplrnn": _b.DEER_SHPLRNN, "diag_ssm": _b.DEER_DIAG_SSM}
 _INITS = {"teacher": _b.DEER_INIT_TEACHER, "zero": _b.DEER_INIT_ZERO, "user": _b.DEER_INIT_USER}
@@ -431,3 +436,228 @@ def deer_scan_noalloc(layout: int, J, b, y, reverse: bool = False, transpose=Non
 def deer_noalloc_scratch_bytes() -> int:
     return int(load().deer_noalloc_scratch_bytes())
 
+
+# ---- linear attention with a decay for each head, layer normalisation ------------------------
+
+_DTYPES = {torch.float32: _b.DEER_F32, torch.bfloat16: _b.DEER_BF16, torch.float16: _b.DEER_F16}
+
+
+def _operand(name, t, ref=None, shape=None, dtype=None):
+    """Checks an argument of a layer (a GPU tensor on ref's GPU, of the given shape and type)."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor")
+    if ref is not None and t.device != ref.device:
+        raise ValueError(f"{name} is on {t.device}, not on {ref.device}")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
+    return t
+
+
+def _result(name, t, ref, shape, dtype):
+    """A caller's output buffer, or a new one."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=ref.device)
+    if not _operand(name, t, ref, shape, dtype).is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t
+
+
+def _view(t):
+    """t (kept alive by the caller) and its view struct: [B, T, heads, D], or [B, heads, D] of one step."""
+    if t.stride(-1) != 1 and t.shape[-1] != 1:
+        t = t.contiguous()
+    s = t.stride()
+    return t, _b.deer_view(t.data_ptr(), s[0], s[1] if t.dim() == 4 else 0, s[-2])
+
+
+class _Lin:
+    """The checked operands of one call of linear attention."""
+
+    def __init__(self, q, k, v, log_decay, scale, lengths):
+        dim = _operand("v", v).dim()
+        if dim not in (3, 4):
+            raise ValueError("v must be [B, T, H, Dv] (a step: [B, H, Dv])")
+        if v.dtype not in _DTYPES:
+            raise ValueError(f"unsupported type {v.dtype}")
+        if _operand("q", q, v, None, v.dtype).dim() != dim:
+            raise ValueError("q must have as many dimensions as v")
+        lead = tuple(v.shape[:-2])
+        self.H, self.Dv = v.shape[-2:]
+        self.Hk, self.Dk = q.shape[-2:]
+        self.lead = lead
+        self.B, self.T = lead[0], lead[1] if dim == 4 else 1
+        _operand("q", q, v, (*lead, self.Hk, self.Dk))
+        _operand("k", k, v, (*lead, self.Hk, self.Dk), v.dtype)
+        _operand("log_decay", log_decay, v, None, torch.float32)
+        per_step = log_decay.dim() > 1
+        _operand("log_decay", log_decay, v, (*lead, self.H) if per_step else (self.H,))
+        if lengths is not None:
+            lengths = _operand("lengths", lengths, v, (self.B,), torch.int32).contiguous()
+        (self.q, self.vq), (self.k, self.vk), (self.v, self.vv) = _view(q), _view(k), _view(v)
+        self.log_decay, self.lengths = log_decay.contiguous(), lengths
+        self.c = _b.deer_linattn_shape(_DTYPES[v.dtype], self.H, self.Hk, self.Dk, self.Dv, int(per_step), float(scale))
+
+    def matrix(self, name, t):
+        """A state or its cotangent, contiguous."""
+        if t is None:
+            return None
+        return _operand(name, t, self.v, (self.B, self.H, self.Dk, self.Dv), torch.float32).contiguous()
+
+    def workspace(self, lib, op):
+        n = lib.deer_linattn_workspace_bytes(ctypes.byref(self.c), self.B, self.T, op)
+        return torch.empty(max(int(n), 256), dtype=torch.uint8, device=self.v.device)
+
+
+def deer_linattn_workspace_bytes(B: int, T: int, H: int, Hk: int, Dk: int, Dv: int, op: int,
+                                 dtype=torch.float32) -> int:
+    """Workspace of deer_linattn (op DEER_OP_SOLVE) or deer_linattn_adjoint (DEER_OP_ADJOINT); 0 for
+    arguments they refuse."""
+    c = _b.deer_linattn_shape(_DTYPES[dtype], H, Hk, Dk, Dv, 0, 1.0)
+    return int(load().deer_linattn_workspace_bytes(ctypes.byref(c), B, T, op))
+
+
+def deer_linattn(q, k, v, log_decay, *, scale: float = 1.0, lengths=None, state0=None, want_state: bool = False, o=None,
+                 state=None, ws=None) -> dict:
+    """Linear attention with a decay for each head over whole sequences:
+    S_t = exp(log_decay_t) S_{t-1} + k_t v_t^T, o_t = scale S_t^T q_t.
+
+    q, k [B, T, Hk, Dk] and v [B, T, H, Dv] (H a multiple of Hk) in float32, bfloat16 or float16, any
+    strides (views with a unit last stride are read in place); log_decay float32 [H] or [B, T, H];
+    lengths int32 [B] (steps of each sequence; rows behind them are not read and give zeros);
+    state0 float32 [B, H, Dk, Dv].  o and state are buffers for the outputs; state may be state0.
+    Returns dict(o [B, T, H, Dv], state (None unless want_state or a buffer is given))."""
+    lib = load()
+    a = _Lin(q, k, v, log_decay, scale, lengths)
+    if v.dim() != 4:
+        raise ValueError("v must be [B, T, H, Dv]")
+    with torch.cuda.device(v.device):
+        o = _result("o", o, v, a.v.shape, v.dtype)
+        s0 = a.matrix("state0", state0)
+        if state is not None or want_state:
+            state = _result("state", state, v, (a.B, a.H, a.Dk, a.Dv), torch.float32)
+        if ws is None:
+            ws = a.workspace(lib, _b.DEER_OP_SOLVE)
+        st = lib.deer_linattn(ctypes.byref(a.c), a.B, a.T, ctypes.byref(a.vq), ctypes.byref(a.vk), ctypes.byref(a.vv),
+                              _ptr(a.log_decay), _ptr(a.lengths), _ptr(s0), _ptr(o), _ptr(state), _ptr(ws), ws.numel(),
+                              _stream())
+    _b._check(st, "deer_linattn")
+    return {"o": o, "state": state}
+
+
+def deer_linattn_adjoint(q, k, v, log_decay, g, *, scale: float = 1.0, lengths=None, state0=None, g_state=None,
+                         want_decay: bool = True, ws=None) -> dict:
+    """Gradients of deer_linattn for the cotangents g of o [B, T, H, Dv] and g_state of the last state
+    (float32 [B, H, Dk, Dv] or None).  Returns dict(grads = {q, k, v, log_decay (with want_decay),
+    state0 (if state0 is given)}); q, k, v in the operands' type, the others in float32."""
+    lib = load()
+    a = _Lin(q, k, v, log_decay, scale, lengths)
+    if v.dim() != 4:
+        raise ValueError("v must be [B, T, H, Dv]")
+    with torch.cuda.device(v.device):
+        gt, vg = _view(_operand("g", g, v, v.shape, v.dtype))
+        s0, gs = a.matrix("state0", state0), a.matrix("g_state", g_state)
+        grads = {"q": torch.empty(q.shape, dtype=q.dtype, device=v.device),
+                 "k": torch.empty(k.shape, dtype=k.dtype, device=v.device),
+                 "v": torch.empty(v.shape, dtype=v.dtype, device=v.device)}
+        if want_decay:
+            grads["log_decay"] = torch.empty(log_decay.shape, device=v.device)
+        if s0 is not None:
+            grads["state0"] = torch.empty(s0.shape, device=v.device)
+        if ws is None:
+            ws = a.workspace(lib, _b.DEER_OP_ADJOINT)
+        st = lib.deer_linattn_adjoint(ctypes.byref(a.c), a.B, a.T, ctypes.byref(a.vq), ctypes.byref(a.vk),
+                                      ctypes.byref(a.vv), _ptr(a.log_decay), _ptr(a.lengths), _ptr(s0),
+                                      ctypes.byref(vg), _ptr(gs), _ptr(grads["q"]), _ptr(grads["k"]), _ptr(grads["v"]),
+                                      _ptr(grads.get("log_decay")), _ptr(grads.get("state0")), _ptr(ws), ws.numel(),
+                                      _stream())
+    _b._check(st, "deer_linattn_adjoint")
+    return {"grads": grads}
+
+
+def deer_linattn_step(q, k, v, log_decay, state, *, scale: float = 1.0, lengths=None, o=None) -> dict:
+    """One step of deer_linattn for every sequence (generation): q, k [B, Hk, Dk], v [B, H, Dv],
+    log_decay [H] or [B, H]; state float32 [B, H, Dk, Dv], contiguous, is updated in place.  A sequence
+    whose entry of lengths (int32 [B]) is 0 takes no step.  Returns dict(o [B, H, Dv], state)."""
+    lib = load()
+    a = _Lin(q, k, v, log_decay, scale, lengths)
+    if v.dim() != 3:
+        raise ValueError("v must be [B, H, Dv]")
+    with torch.cuda.device(v.device):
+        state = _result("state", _operand("state", state), v, (a.B, a.H, a.Dk, a.Dv), torch.float32)
+        o = _result("o", o, v, a.v.shape, v.dtype)
+        st = lib.deer_linattn_step(ctypes.byref(a.c), a.B, ctypes.byref(a.vq), ctypes.byref(a.vk), ctypes.byref(a.vv),
+                                   _ptr(a.log_decay), _ptr(a.lengths), _ptr(state), _ptr(o), _stream())
+    _b._check(st, "deer_linattn_step")
+    return {"o": o, "state": state}
+
+
+def _norm(x, w, b, eps):
+    """Contiguous x, w, b, the row count and the C struct: weights [D], or [G, D] for x [..., G, D]."""
+    _operand("x", x)
+    if x.dtype not in _DTYPES:
+        raise ValueError(f"unsupported type {x.dtype}")
+    if x.dim() < 1:
+        raise ValueError("x must have at least one dimension")
+    given = w if w is not None else b
+    G, wtype = 1, _b.DEER_F32
+    if given is not None:
+        _operand("w" if w is not None else "b", given, x)
+        if given.dtype not in (torch.float32, x.dtype):
+            raise ValueError(f"w and b must be float32 or {x.dtype}, not {given.dtype}")
+        if given.dim() not in (1, 2) or tuple(given.shape) != tuple(x.shape[x.dim() - given.dim():]):
+            raise ValueError(f"w and b must have the shape of x's last or last two dimensions, not {tuple(given.shape)}")
+        if b is not None:
+            _operand("b", b, x, given.shape, given.dtype)
+        G = given.shape[0] if given.dim() == 2 else 1
+        wtype = _DTYPES[given.dtype]
+    x = x.contiguous()
+    w, b = (None if t is None else t.contiguous() for t in (w, b))
+    D = x.shape[-1]
+    rows = x.numel() // D if D else 0
+    return x, w, b, rows, _b.deer_norm(_DTYPES[x.dtype], wtype, G, D, _ptr(w), _ptr(b), float(eps))
+
+
+def deer_layernorm_workspace_bytes(rows: int, G: int, D: int, dtype=torch.float32) -> int:
+    """Workspace of deer_layernorm_adjoint; 0 for arguments it refuses."""
+    c = _b.deer_norm(_DTYPES[dtype], _b.DEER_F32, G, D, None, None, 0.0)
+    return int(load().deer_layernorm_workspace_bytes(ctypes.byref(c), rows))
+
+
+def deer_layernorm(x, w=None, b=None, *, eps: float = 1e-5, y=None) -> dict:
+    """Layer normalisation over the last dimension of x (float32, bfloat16 or float16):
+    y = (x - mean) rstd w + b.  w, b: [D], or [G, D] with x [..., G, D] (weights of its own for each
+    head), float32 or x's type, or None.  Returns dict(y, mean, rstd), the statistics in float32."""
+    lib = load()
+    xc, wc, bc, rows, c = _norm(x, w, b, eps)
+    with torch.cuda.device(x.device):
+        y = _result("y", y, x, x.shape, x.dtype)
+        mean = torch.empty(x.shape[:-1], device=x.device)
+        rstd = torch.empty(x.shape[:-1], device=x.device)
+        st = lib.deer_layernorm(ctypes.byref(c), rows, _ptr(xc), _ptr(y), _ptr(mean), _ptr(rstd), _stream())
+    _b._check(st, "deer_layernorm")
+    return {"y": y, "mean": mean, "rstd": rstd}
+
+
+def deer_layernorm_adjoint(x, g, mean, rstd, w=None, *, want_grads: bool = True, ws=None) -> dict:
+    """Gradients of deer_layernorm for the cotangent g of y, with its mean and rstd.  Returns dict(x =
+    dL/dx in x's type, grads = {w, b} in float32, of w's shape ([D] without w); {} without want_grads)."""
+    lib = load()
+    xc, wc, _, rows, c = _norm(x, w, None, 0.0)
+    with torch.cuda.device(x.device):
+        gc = _operand("g", g, x, x.shape, x.dtype).contiguous()
+        mc = _operand("mean", mean, x, x.shape[:-1], torch.float32).contiguous()
+        rc = _operand("rstd", rstd, x, x.shape[:-1], torch.float32).contiguous()
+        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        grads = {}
+        if want_grads:
+            shape = x.shape[-1:] if w is None else w.shape
+            grads = {"w": torch.empty(shape, device=x.device), "b": torch.empty(shape, device=x.device)}
+        if ws is None:
+            n = lib.deer_layernorm_workspace_bytes(ctypes.byref(c), rows)
+            ws = torch.empty(max(int(n), 256), dtype=torch.uint8, device=x.device)
+        st = lib.deer_layernorm_adjoint(ctypes.byref(c), rows, _ptr(xc), _ptr(gc), _ptr(mc), _ptr(rc), _ptr(dx),
+                                        _ptr(grads.get("w")), _ptr(grads.get("b")), _ptr(ws), ws.numel(), _stream())
+    _b._check(st, "deer_layernorm_adjoint")
+    return {"x": dx, "grads": grads}

@@ -20,6 +20,7 @@ DEER_INIT_TEACHER, DEER_INIT_ZERO, DEER_INIT_USER = 0, 1, 2
 DEER_OP_SOLVE, DEER_OP_ADJOINT, DEER_OP_JACOBIAN = 0, 1, 2
 DEER_SCAN_DENSE, DEER_SCAN_DIAG_C64 = 0, 1
 DEER_G_NATIVE, DEER_G_REAL = 0, 1
+DEER_F32, DEER_BF16, DEER_F16 = 0, 1, 2
 
 EXPORTED = ["deer_workspace_bytes", "deer_solve", "deer_adjoint", "deer_adjoint_ex", "plrnn_jacobian", "deer_scan",
             "deer_scan_workspace_bytes", "deer_readout_workspace_bytes", "deer_readout_loss", "deer_status_string",
@@ -27,7 +28,8 @@ EXPORTED = ["deer_workspace_bytes", "deer_solve", "deer_adjoint", "deer_adjoint_
             "deer_quasi_workspace_bytes", "deer_sequential", "deer_sequential_workspace_bytes",
             "deer_workspace_bytes_ex", "deer_train_step", "deer_train_workspace_bytes", "deer_train_params",
             "deer_host_reserve", "deer_host_release", "deer_scan_noalloc", "deer_noalloc_scratch_bytes",
-            "plrnn_jacobian_ex"]
+            "plrnn_jacobian_ex", "deer_linattn_workspace_bytes", "deer_linattn", "deer_linattn_adjoint",
+            "deer_linattn_step", "deer_layernorm", "deer_layernorm_adjoint", "deer_layernorm_workspace_bytes"]
 
 _fp = ctypes.c_void_p
 
@@ -63,6 +65,20 @@ class deer_readout(ctypes.Structure):
 
 class deer_readout_grads(ctypes.Structure):
     _fields_ = [("Wa", _fp), ("ca", _fp), ("Wb", _fp), ("cb", _fp)]
+
+
+class deer_linattn_shape(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("H", ctypes.c_int), ("Hk", ctypes.c_int), ("Dk", ctypes.c_int),
+                ("Dv", ctypes.c_int), ("per_step", ctypes.c_int), ("scale", ctypes.c_float)]
+
+
+class deer_view(ctypes.Structure):
+    _fields_ = [("p", _fp), ("sb", ctypes.c_int64), ("st", ctypes.c_int64), ("sh", ctypes.c_int64)]
+
+
+class deer_norm(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("wtype", ctypes.c_int), ("G", ctypes.c_int), ("D", ctypes.c_int),
+                ("w", _fp), ("b", _fp), ("eps", ctypes.c_float)]
 
 
 _lib = None
@@ -127,6 +143,22 @@ def load(path: str = LIB_PATH):
     lib.deer_scan_noalloc.restype = i32
     lib.deer_noalloc_scratch_bytes.argtypes = []
     lib.deer_noalloc_scratch_bytes.restype = sz
+    shape, view, norm, i64 = P(deer_linattn_shape), P(deer_view), P(deer_norm), ctypes.c_int64
+    lib.deer_linattn_workspace_bytes.argtypes = [shape, i32, i32, i32]
+    lib.deer_linattn_workspace_bytes.restype = sz
+    lib.deer_linattn.argtypes = [shape, i32, i32, view, view, view, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.deer_linattn.restype = i32
+    lib.deer_linattn_adjoint.argtypes = [shape, i32, i32, view, view, view, vp, vp, vp, view, vp, vp, vp, vp, vp, vp,
+                                         vp, sz, vp]
+    lib.deer_linattn_adjoint.restype = i32
+    lib.deer_linattn_step.argtypes = [shape, i32, view, view, view, vp, vp, vp, vp, vp]
+    lib.deer_linattn_step.restype = i32
+    lib.deer_layernorm.argtypes = [norm, i64, vp, vp, vp, vp, vp]
+    lib.deer_layernorm.restype = i32
+    lib.deer_layernorm_adjoint.argtypes = [norm, i64, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.deer_layernorm_adjoint.restype = i32
+    lib.deer_layernorm_workspace_bytes.argtypes = [norm, i64]
+    lib.deer_layernorm_workspace_bytes.restype = sz
     lib.deer_host_reserve.argtypes = [i32]
     lib.deer_host_reserve.restype = i32
     lib.deer_host_release.argtypes = []

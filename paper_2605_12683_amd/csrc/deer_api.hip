@@ -171,18 +171,6 @@ int launch_fill_f32(float *p, size_t n, float v, hipStream_t st) {
 }
 
 // ---- workspace carving ---------------------------------------------------------------------
-struct Carver {
-    char *base;
-    size_t off = 0;
-    explicit Carver(void *b) : base((char *)b) {}
-    template <class Tp>
-    Tp *take(size_t count) {
-        Tp *p = base ? (Tp *)(base + off) : nullptr;
-        off += (count * sizeof(Tp) + 255) & ~(size_t)255;
-        return p;
-    }
-};
-
 static int chunk_override() {
     const char *e = getenv("DEER_CHUNK");
     return e ? atoi(e) : 0;
@@ -573,7 +561,7 @@ static int check_quasi(const deer_model *m, const deer_forcing *f, int B, int T)
     return DEER_OK;
 }
 
-static int check_ws(void *ws, size_t have, size_t need) {
+int check_ws(void *ws, size_t have, size_t need) {
     if (need == 0) return DEER_OK;
     if (!ws || have < need) {
         set_error("workspace too small: need %zu bytes, have %zu", need, ws ? have : (size_t)0);

@@ -4,6 +4,21 @@
 
 namespace deer {
 
+// ---- workspace carving and checks (C-ABI layer) --------------------------------------------
+// 256-byte aligned pieces of a caller's workspace; with a null base only the size is counted
+struct Carver {
+    char *base;
+    size_t off = 0;
+    explicit Carver(void *b) : base((char *)b) {}
+    template <class Tp>
+    Tp *take(size_t count) {
+        Tp *p = base ? (Tp *)(base + off) : nullptr;
+        off += (count * sizeof(Tp) + 255) & ~(size_t)255;
+        return p;
+    }
+};
+int check_ws(void *ws, size_t have, size_t need);
+
 struct FusedCtl;   // pass-end control fused into a pass kernel (defined below)
 
 struct PlrnnArgs {
@@ -311,6 +326,70 @@ int launch_obs_bgrad(const float *JF, const float *lam, const float *z, const fl
                      const double *Bp64, const double *Bm64, const double *P164, bool z0_given, float alpha, int T_w,
                      bool with_mse, double mse_scale, int B, int T, int M, int N, double *ws, float *gB,
                      hipStream_t st);
+
+// linear attention with decays (k_linattn.hip): operands element [b, t, h, d] at p + b sb + t st + h sh + d
+struct LinView {
+    const void *p;
+    long sb, st, sh;
+    int r;                      // heads of the result that share one head of this operand
+};
+// one walk of the recurrence S = exp(gate) S + sc_kv k v^T, out = sc_o q^T S over [B, T, H]: the
+// forward pass and each gradient of its adjoint are walks with the operands in other places
+struct LinRole {
+    LinView q, k, v;            // q, k: Kd wide; v: N wide
+    int Kd, N;
+    bool reverse;               // t from T - 1 to 0, the decay of step t applied on the way to t - 1
+    float sc_kv, sc_o;
+    void *out;                  // [B, T, H, N]
+    bool out_f32;               // float32 whatever the operands' type
+    const float *init;          // state before the first step, or null (zero): [B, H] matrices of
+    int init_d, init_n;         // Kd N floats, element (d, n) at d init_d + n init_n
+    float *fin;                 // state after the last step (reverse: times exp of step 0's decay), or null
+    int fin_d, fin_n;
+    LinView partner;            // N wide, or p = null: dot[b, h, t] = <partner row, out row>
+    float *dot;                 // [tiles][B, H, T]
+    float *anchor;              // [B, H, anchors][Kd, N] or null: the state at every kLinAnchor steps
+};
+constexpr int kLinAnchor = 1024;   // steps between the states kept for the gradient of the decays
+struct LinArgs {
+    int dtype, B, T, H;
+    const float *log_decay;     // [H], or [B, T, H] with per_step
+    bool per_step;
+    const int32_t *lengths;     // [B] or null
+};
+int lin_tiles(int Kd, int N);
+int launch_lin_walk(const LinArgs &a, const LinRole *roles, int nroles, hipStream_t st);
+// gradient of the log decays from the dots of dq and dk and the states at the anchors:
+// part is [B, H, anchors] doubles
+int launch_lin_decay_grad(const LinArgs &a, const float *dq_dot, int q_tiles, const float *dk_dot, int k_tiles,
+                          const float *fwd_anchor, const float *rev_anchor, int elems, double *part, float *dlog_decay,
+                          hipStream_t st);
+// out[b, t, hk, :] = sum over the r heads that share hk of in[b, t, hk r + i, :]
+int launch_lin_head_sum(int dtype, size_t rows, int Hk, int r, int D, const float *in, void *out, hipStream_t st);
+struct LinStep {
+    int dtype, B, H, Hk, Dk, Dv;
+    bool per_seq;               // log_decay [B, H] instead of [H]
+    float scale;
+    LinView q, k, v;            // st unused
+    const float *log_decay;
+    const int32_t *lengths;
+    float *state;
+    void *o;
+};
+int launch_lin_step(const LinStep &a, hipStream_t st);
+
+// layer normalisation (k_norm.hip): rows of D elements, weights [G, D], row i uses row i % G
+struct NormArgs {
+    int dtype, wtype;
+    size_t rows;
+    int G, D;
+    const void *x, *w, *b;
+    float eps;
+};
+int launch_layernorm(const NormArgs &a, void *y, float *mean, float *rstd, hipStream_t st);
+size_t layernorm_adjoint_ws_bytes(size_t rows, int G, int D);
+int launch_layernorm_adjoint(const NormArgs &a, const void *g, const float *mean, const float *rstd, void *dx,
+                             float *dw, float *db, void *ws, hipStream_t st);
 
 // small utilities
 int launch_fill_teacher(int B, int T, int M, int N, const float *x, float *z, hipStream_t st);
