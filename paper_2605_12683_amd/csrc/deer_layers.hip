@@ -41,8 +41,24 @@ static int check_alias(const void *out, const char *name, const void *const *in,
 
 static LinView view_of(const deer_view *x, int r) { return {x->p, (long)x->sb, (long)x->st, (long)x->sh, r}; }
 
-static LinArgs args_of(const deer_linattn_shape *s, int B, int T, const float *log_decay, const int32_t *lengths) {
-    return {s->dtype, B, T, s->H, log_decay, s->per_step != 0, lengths};
+// Segments: enough that the walks' blocks fill the chip twice (two blocks share a CU), none of
+// fewer than kMinSeg steps; one where the walks alone give half of that, since further segments
+// read k and v a second time.
+constexpr int kFillBlocks = 512, kMinSeg = 256;
+
+static int segment_steps(const deer_linattn_shape *s, int B, int T, int op) {
+    long blocks = (long)B * s->H * lin_tiles(s->dtype, s->Dk, s->Dv);
+    if (op == DEER_OP_ADJOINT) blocks += 2L * B * s->H * lin_tiles(s->dtype, s->Dv, s->Dk);
+    if (2 * blocks >= kFillBlocks || T <= kMinSeg) return T;
+    const long n = (kFillBlocks + blocks - 1) / blocks;
+    const long steps = ((T + n - 1) / n + 63) / 64 * 64;
+    return (int)(steps < kMinSeg ? kMinSeg : steps);
+}
+
+static LinArgs args_of(const deer_linattn_shape *s, int B, int T, int op, const float *log_decay,
+                       const int32_t *lengths) {
+    const int steps = segment_steps(s, B, T, op);
+    return {s->dtype, B, T, s->H, log_decay, s->per_step != 0, lengths, steps, (T + steps - 1) / steps};
 }
 
 struct LinWs {
@@ -50,6 +66,8 @@ struct LinWs {
     float *dq_dot, *dk_dot;      // [tiles][B, H, T]
     float *fwd, *rev;            // states at the anchors [B, H, anchors][Dv, Dk]
     double *part;                // [B, H, anchors]
+    float *seg, *seg_decay;      // [B, H, segments] of the forward state (the adjoint: S^T) ...
+    float *rseg, *rseg_decay;    // ... and of R
     size_t bytes;
 };
 
@@ -63,15 +81,29 @@ static LinWs carve_lin(void *ws, const deer_linattn_shape *s, int B, int T, int 
             w.dq = c.take<float>(bh * T * s->Dk);
             w.dk = c.take<float>(bh * T * s->Dk);
         }
-        const int tiles = lin_tiles(s->Dv, s->Dk);
+        const int tiles = lin_tiles(s->dtype, s->Dv, s->Dk);
         w.dq_dot = c.take<float>(tiles * bh * T);
         w.dk_dot = c.take<float>(tiles * bh * T);
         w.fwd = c.take<float>(bh * na * s->Dk * s->Dv);
         w.rev = c.take<float>(bh * na * s->Dk * s->Dv);
         w.part = c.take<double>(bh * na);
     }
+    const int steps = segment_steps(s, B, T, op);
+    if (steps < T) {
+        const size_t n = (size_t)B * s->H * ((T + steps - 1) / steps);
+        w.seg = c.take<float>(n * s->Dk * s->Dv);
+        w.seg_decay = c.take<float>(n);
+        if (op == DEER_OP_ADJOINT) {
+            w.rseg = c.take<float>(n * s->Dk * s->Dv);
+            w.rseg_decay = c.take<float>(n);
+        }
+    }
     w.bytes = c.off;
     return w;
+}
+
+static bool wide_out(const void *p, int dtype, int N) {
+    return N % 4 == 0 && ((uintptr_t)p & (4 * dtype_size(dtype) - 1)) == 0;
 }
 
 static int check_norm(const deer_norm *n, int64_t rows) {
@@ -117,15 +149,22 @@ int deer_linattn(const deer_linattn_shape *s, int B, int T, const deer_view *q, 
     if ((rc = check_alias(o, "o", in, 5)) || (rc = check_alias(state, "state", in, 4))) return rc;
     if (state && (void *)state == o) { set_error("o and state may not be the same memory"); return DEER_ERR_INVALID_ARG; }
     if ((rc = check_ws(ws, ws_bytes, carve_lin(nullptr, s, B, T, DEER_OP_SOLVE).bytes))) return rc;
+    const LinWs w = carve_lin(ws, s, B, T, DEER_OP_SOLVE);
+    const LinArgs a = args_of(s, B, T, DEER_OP_SOLVE, log_decay, lengths);
+    hipStream_t st = (hipStream_t)stream;
     const int r = s->H / s->Hk;
     LinRole ro{};
     ro.q = view_of(q, r), ro.k = view_of(k, r), ro.v = view_of(v, 1);
     ro.Kd = s->Dk, ro.N = s->Dv;
     ro.sc_kv = 1.f, ro.sc_o = s->scale;
-    ro.out = o;
+    ro.out = o, ro.wide_out = wide_out(o, s->dtype, s->Dv);
     ro.init = state0, ro.init_d = s->Dv, ro.init_n = 1;
     ro.fin = state, ro.fin_d = s->Dv, ro.fin_n = 1;
-    return launch_lin_walk(args_of(s, B, T, log_decay, lengths), &ro, 1, (hipStream_t)stream);
+    if (a.nseg > 1) {
+        ro.seg = w.seg, ro.seg_decay = w.seg_decay, ro.seg_d = s->Dv, ro.seg_n = 1;
+        if ((rc = launch_lin_walk(a, &ro, 1, true, false, st)) || (rc = launch_lin_join(a, &ro, 1, st))) return rc;
+    }
+    return launch_lin_walk(a, &ro, 1, false, false, st);
 }
 
 int deer_linattn_adjoint(const deer_linattn_shape *s, int B, int T, const deer_view *q, const deer_view *k,
@@ -156,7 +195,7 @@ int deer_linattn_adjoint(const deer_linattn_shape *s, int B, int T, const deer_v
     ro[0].q = vg, ro[0].k = vv, ro[0].v = vk;
     ro[0].Kd = Dv, ro[0].N = Dk;
     ro[0].sc_kv = 1.f, ro[0].sc_o = s->scale;
-    ro[0].out = shared ? (void *)w.dq : dq, ro[0].out_f32 = shared;
+    ro[0].out = shared ? (void *)w.dq : dq, ro[0].out_f32 = shared, ro[0].wide_out = wide_out(dq, s->dtype, Dk);
     ro[0].init = state0, ro[0].init_d = 1, ro[0].init_n = Dv;
     if (decay) ro[0].partner = vq, ro[0].dot = w.dq_dot, ro[0].anchor = w.fwd;
     // dk: the state is R^T [Dv, Dk]
@@ -164,7 +203,7 @@ int deer_linattn_adjoint(const deer_linattn_shape *s, int B, int T, const deer_v
     ro[1].Kd = Dv, ro[1].N = Dk;
     ro[1].reverse = true;
     ro[1].sc_kv = s->scale, ro[1].sc_o = 1.f;
-    ro[1].out = shared ? (void *)w.dk : dk, ro[1].out_f32 = shared;
+    ro[1].out = shared ? (void *)w.dk : dk, ro[1].out_f32 = shared, ro[1].wide_out = wide_out(dk, s->dtype, Dk);
     ro[1].init = g_state, ro[1].init_d = 1, ro[1].init_n = Dv;
     if (decay) ro[1].partner = vk, ro[1].dot = w.dk_dot, ro[1].anchor = w.rev;
     // dv: the state is R [Dk, Dv]
@@ -172,19 +211,38 @@ int deer_linattn_adjoint(const deer_linattn_shape *s, int B, int T, const deer_v
     ro[2].Kd = Dk, ro[2].N = Dv;
     ro[2].reverse = true;
     ro[2].sc_kv = s->scale, ro[2].sc_o = 1.f;
-    ro[2].out = dv;
+    ro[2].out = dv, ro[2].wide_out = wide_out(dv, s->dtype, Dv);
     ro[2].init = g_state, ro[2].init_d = Dv, ro[2].init_n = 1;
     ro[2].fin = dstate0, ro[2].fin_d = Dv, ro[2].fin_n = 1;
-    const LinArgs a = args_of(s, B, T, log_decay, lengths);
+    const LinArgs a = args_of(s, B, T, DEER_OP_ADJOINT, log_decay, lengths);
     hipStream_t st = (hipStream_t)stream;
-    if ((rc = launch_lin_walk(a, ro, 3, st))) return rc;
+    const bool same = lin_same_tile(s->dtype, Dv, Dk, Dk, Dv);
+    if (a.nseg > 1) {
+        ro[0].seg = w.seg, ro[0].seg_decay = w.seg_decay, ro[0].seg_d = Dk, ro[0].seg_n = 1;
+        ro[2].seg = w.rseg, ro[2].seg_decay = w.rseg_decay, ro[2].seg_d = Dv, ro[2].seg_n = 1;
+        const LinRole two[2] = {ro[0], ro[2]};
+        if (same) {
+            if ((rc = launch_lin_walk(a, two, 2, true, false, st))) return rc;
+        } else if ((rc = launch_lin_walk(a, two, 1, true, false, st)) ||
+                   (rc = launch_lin_walk(a, two + 1, 1, true, false, st))) {
+            return rc;
+        }
+        if ((rc = launch_lin_join(a, two, 2, st))) return rc;
+        ro[1].seg = w.rseg, ro[1].seg_d = 1, ro[1].seg_n = Dv;   // R^T: the same states, read across
+    }
+    // dots that are summed over up to kLinAnchor steps take the finer products
+    if (same && !decay) {
+        if ((rc = launch_lin_walk(a, ro, 3, false, false, st))) return rc;
+    } else if ((rc = launch_lin_walk(a, ro, 2, false, decay, st)) || (rc = launch_lin_walk(a, ro + 2, 1, false, false, st))) {
+        return rc;
+    }
     if (shared) {
         const size_t rows = (size_t)B * T;
         if ((rc = launch_lin_head_sum(s->dtype, rows, s->Hk, r, Dk, w.dq, dq, st))) return rc;
         if ((rc = launch_lin_head_sum(s->dtype, rows, s->Hk, r, Dk, w.dk, dk, st))) return rc;
     }
     if (!decay) return DEER_OK;
-    const int tiles = lin_tiles(Dv, Dk);
+    const int tiles = lin_tiles(s->dtype, Dv, Dk);
     return launch_lin_decay_grad(a, w.dq_dot, tiles, w.dk_dot, tiles, w.fwd, w.rev, Dk * Dv, w.part, dlog_decay, st);
 }
 

@@ -6,116 +6,80 @@
 //   o  : q, k, v  forwards                 dq : g, v, k  forwards (the state is S^T)
 //   dv : k, q, g  backwards (state R)      dk : v, g, q  backwards (state R^T)
 // so one kernel computes them all (LinRole).
-#include "launch.h"
-#include "types16.h"
+#include "linwalk.h"
 
 namespace deer {
 
-constexpr double kLog2e = 1.4426950408889634074;
+// ---- walks in segments ----------------------------------------------------------------------------
+//
+// With few heads the walks alone do not fill the chip, so a sequence is cut into segments: a first
+// walk finds the state that each adds by itself, k_lin_join turns these into the state entering
+// each (one pass over the segments, in place), and the walks proper start from there, all at once.
+// That reads k and v twice.
 
-// log2 of the decay of a step.  Below 2^-256 a decay is zero in float32 whatever it multiplies
-// by less than 2^107, and a bounded exponent keeps the differences of sums finite (-inf: a state
-// that starts anew).  A NaN stays one.
-__device__ __forceinline__ double gate_of(float log_decay) {
-    const double g = (double)log_decay * kLog2e;
-    return g < -256.0 ? -256.0 : g;
-}
-
-// log2 of the factor the walk applies to its state on entering step t: forwards the decay of t,
-// backwards that of t + 1; one behind the sequence's end
-__device__ __forceinline__ double gate_at(const LinArgs &a, int b, int h, int t, int len, bool rev) {
-    const int s = rev ? t + 1 : t;
-    if (s >= len) return 0.0;
-    return gate_of(a.per_step ? a.log_decay[((size_t)b * a.T + s) * a.H + h] : a.log_decay[h]);
-}
-
-__device__ __forceinline__ int length_of(const LinArgs &a, int b) {
-    if (!a.lengths) return a.T;
-    const int n = a.lengths[b];
-    return n < 0 ? 0 : (n > a.T ? a.T : n);
-}
-
-template <class Ty>
-__device__ __forceinline__ const typename Ty::T *row_of(const LinView &x, int b, int t, int h) {
-    return (const typename Ty::T *)x.p + b * x.sb + t * x.st + (h / x.r) * x.sh;
-}
-
-// ---- the walk ---------------------------------------------------------------------------------
-
-constexpr int kTile = 64;   // columns of the state per block
-
-int lin_tiles(int Kd, int N) { return (N + kTile - 1) / kTile; }
-
-// One wave per 64 columns of one head's state, which lies in LDS; one step after the other.
-template <class Ty>
-__global__ __launch_bounds__(64) void k_lin_walk(LinArgs a, LinRole ro) {
-    extern __shared__ float lds[];
-    float *S = lds;                    // [Kd][64]
-    float *qs = S + ro.Kd * kTile, *ks = qs + ro.Kd;
-    const int tiles = (ro.N + kTile - 1) / kTile;
-    const int tile = blockIdx.x % tiles, bh = blockIdx.x / tiles;
-    const int b = bh / a.H, h = bh % a.H, lane = threadIdx.x, n = tile * kTile + lane;
-    const bool on = n < ro.N;
-    const int len = length_of(a, b);
-    const size_t mat = (size_t)ro.Kd * ro.N;
-    for (int d = 0; d < ro.Kd; ++d)
-        S[d * kTile + lane] = ro.init && on ? ro.init[bh * mat + (size_t)d * ro.init_d + (size_t)n * ro.init_n] : 0.f;
-    const int na = (a.T + kLinAnchor - 1) / kLinAnchor;
-    for (int i = 0; i < a.T; ++i) {
-        const int t = ro.reverse ? a.T - 1 - i : i;
-        const bool edge = (t + 1) % kLinAnchor == 0 || t + 1 == a.T;
-        float *anc = ro.anchor && edge ? ro.anchor + ((size_t)bh * na + t / kLinAnchor) * mat : nullptr;
-        if (anc && ro.reverse && on)
-            for (int d = 0; d < ro.Kd; ++d) anc[(size_t)d * ro.N + n] = S[d * kTile + lane];
-        float o = 0.f;
-        if (t < len) {
-            const typename Ty::T *q = row_of<Ty>(ro.q, b, t, h), *k = row_of<Ty>(ro.k, b, t, h);
-            for (int d = lane; d < ro.Kd; d += 64) qs[d] = Ty::up(q[d]), ks[d] = Ty::up(k[d]);
-            __syncthreads();
-            const float g = exp2f((float)gate_at(a, b, h, t, len, ro.reverse));
-            const float v = on ? ro.sc_kv * Ty::up(row_of<Ty>(ro.v, b, t, h)[n]) : 0.f;
-            for (int d = 0; d < ro.Kd; ++d) {
-                const float s = fmaf(ks[d], v, g * S[d * kTile + lane]);
-                S[d * kTile + lane] = s;
-                o = fmaf(qs[d], s, o);
-            }
-            o *= ro.sc_o;
-            __syncthreads();
+// one element of one head's state per thread, the segments in the walk's order
+__global__ __launch_bounds__(256) void k_lin_join(LinArgs a, LinRoles rs) {
+    const LinRole &ro = rs.r[blockIdx.y];
+    const int mat = ro.Kd * ro.N, per = (mat + 255) / 256;
+    const int bh = blockIdx.x / per, e = blockIdx.x % per * 256 + threadIdx.x;
+    if (bh >= a.B * a.H || e >= mat) return;
+    const int b = bh / a.H, h = bh % a.H, d = e / ro.N, n = e % ro.N;
+    float S = ro.init ? ro.init[(size_t)bh * mat + (size_t)d * ro.init_d + (size_t)n * ro.init_n] : 0.f;
+    float *seg = ro.seg + (size_t)bh * a.nseg * mat + e;
+    const float *dec = ro.seg_decay + (size_t)bh * a.nseg;
+    constexpr int U = 8;
+    for (int i0 = 0; i0 < a.nseg; i0 += U) {
+        float x[U], f[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u, s = ro.reverse ? a.nseg - 1 - i : i;
+            const bool on = i < a.nseg - 1 || (i == a.nseg - 1 && ro.fin);
+            x[u] = on ? seg[(size_t)s * mat] : 0.f;
+            f[u] = on ? dec[s] : 0.f;
         }
-        if (on) {
-            const size_t at = (((size_t)b * a.T + t) * a.H + h) * ro.N + n;
-            if (ro.out_f32) ((float *)ro.out)[at] = o;
-            else ((typename Ty::T *)ro.out)[at] = Ty::down(o);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u, s = ro.reverse ? a.nseg - 1 - i : i;
+            if (i >= a.nseg) break;
+            seg[(size_t)s * mat] = S;
+            S = fmaf(f[u], S, x[u]);
         }
-        if (ro.dot) {
-            float p = on && t < len ? o * Ty::up(row_of<Ty>(ro.partner, b, t, h)[n]) : 0.f;
-            for (int off = 32; off > 0; off >>= 1) p += __shfl_xor(p, off, 64);
-            if (lane == 0) ro.dot[((size_t)tile * a.B * a.H + bh) * a.T + t] = p;
-        }
-        if (anc && !ro.reverse && on)
-            for (int d = 0; d < ro.Kd; ++d) anc[(size_t)d * ro.N + n] = S[d * kTile + lane];
     }
-    if (ro.fin && on) {
-        const float g = ro.reverse ? exp2f((float)gate_at(a, b, h, -1, len, true)) : 1.f;
-        for (int d = 0; d < ro.Kd; ++d)
-            ro.fin[bh * mat + (size_t)d * ro.fin_d + (size_t)n * ro.fin_n] = g * S[d * kTile + lane];
-    }
+    if (!ro.fin) return;
+    const float f = ro.reverse ? __builtin_amdgcn_exp2f((float)gate_of(gate_raw(a, b, h, -1, length_of(a, b), true))) : 1.f;
+    ro.fin[(size_t)bh * mat + (size_t)d * ro.fin_d + (size_t)n * ro.fin_n] = f * S;
 }
 
-int launch_lin_walk(const LinArgs &a, const LinRole *roles, int nroles, hipStream_t st) {
-    return with_dtype(a.dtype, [&](auto ty) {
-        using Ty = decltype(ty);
-        for (int i = 0; i < nroles; ++i) {
-            const LinRole &ro = roles[i];
-            const size_t lds = ((size_t)ro.Kd * kTile + 2 * ro.Kd) * sizeof(float);
-            DEER_HIP(hipFuncSetAttribute((const void *)k_lin_walk<Ty>, hipFuncAttributeMaxDynamicSharedMemorySize,
-                                         (int)lds));
-            KTimer kt("k_lin_walk", st);
-            hipLaunchKernelGGL(k_lin_walk<Ty>, dim3(a.B * a.H * lin_tiles(ro.Kd, ro.N)), dim3(64), lds, st, a, ro);
-            DEER_LAUNCH_CHECK("k_lin_walk");
-        }
-        return (int)DEER_OK;
-    });
+int launch_lin_join(const LinArgs &a, const LinRole *roles, int nroles, hipStream_t st) {
+    LinRoles rs{};
+    int most = 0;
+    for (int i = 0; i < nroles; ++i) {
+        rs.r[i] = roles[i];
+        const int n = (roles[i].Kd * roles[i].N + 255) / 256;
+        most = n > most ? n : most;
+    }
+    KTimer kt("k_lin_join", st);
+    hipLaunchKernelGGL(k_lin_join, dim3((unsigned)(a.B * a.H * most), nroles), dim3(256), 0, st, a, rs);
+    DEER_LAUNCH_CHECK("k_lin_join");
+    return DEER_OK;
+}
+
+static int parts_of(int dtype) { return dtype == DEER_F32 ? 3 : dtype == DEER_F16 ? 2 : 1; }
+
+int lin_tiles(int dtype, int Kd, int N) {
+    const int nb = 4 * cw_of(parts_of(dtype), kt_of(Kd), N);
+    return (N + nb - 1) / nb;
+}
+
+bool lin_same_tile(int dtype, int Kd, int N, int Kd2, int N2) {
+    const int p = parts_of(dtype);
+    return kt_of(Kd) == kt_of(Kd2) && cw_of(p, kt_of(Kd), N) == cw_of(p, kt_of(Kd2), N2);
+}
+
+int launch_lin_walk(const LinArgs &a, const LinRole *roles, int nroles, bool states, bool fine, hipStream_t st) {
+    if (a.dtype == DEER_F32) return launch_lin_walk_f32(a, roles, nroles, states, fine, st);
+    if (a.dtype == DEER_BF16) return launch_lin_walk_bf16(a, roles, nroles, states, fine, st);
+    return launch_lin_walk_f16(a, roles, nroles, states, fine, st);
 }
 
 // ---- the gradient of the log decays --------------------------------------------------------------
@@ -147,7 +111,7 @@ __global__ __launch_bounds__(kSpanThreads) void k_lin_decay_grad(LinArgs a, cons
         if (tid < n) sh[tid] += sh[tid + n];
         __syncthreads();
     }
-    z = sh[0] * (double)exp2f((float)gate_at(a, b, h, t1 - 1, len, true));
+    z = sh[0] * (double)__builtin_amdgcn_exp2f((float)gate_of(gate_raw(a, b, h, t1 - 1, len, true)));
     __syncthreads();
     const size_t plane = (size_t)a.B * a.H * a.T;
     double d[kPer], run = 0.0;
@@ -252,6 +216,11 @@ int launch_lin_head_sum(int dtype, size_t rows, int Hk, int r, int D, const floa
 
 // ---- one step ----------------------------------------------------------------------------------------
 
+template <class Ty>
+__device__ __forceinline__ const typename Ty::T *row_of(const LinView &x, int b, int h) {
+    return (const typename Ty::T *)x.p + b * x.sb + (h / x.r) * x.sh;
+}
+
 // One block per 64 columns of one head's state; a thread owns one column of every 4th row.
 template <class Ty>
 __global__ __launch_bounds__(256) void k_lin_step(LinStep a) {
@@ -264,13 +233,13 @@ __global__ __launch_bounds__(256) void k_lin_step(LinStep a) {
         if (w == 0 && on) *o = Ty::down(0.f);
         return;
     }
-    const typename Ty::T *q = row_of<Ty>(a.q, b, 0, h), *k = row_of<Ty>(a.k, b, 0, h);
+    const typename Ty::T *q = row_of<Ty>(a.q, b, h), *k = row_of<Ty>(a.k, b, h);
     for (int d = threadIdx.x; d < a.Dk; d += 256) qs[d] = Ty::up(q[d]), ks[d] = Ty::up(k[d]);
     __syncthreads();
-    const float g = exp2f((float)gate_of(a.log_decay[a.per_seq ? (size_t)bh : h]));
+    const float g = __builtin_amdgcn_exp2f((float)gate_of(a.log_decay[a.per_seq ? (size_t)bh : h]));
     float acc = 0.f;
     if (on) {
-        const float v = Ty::up(row_of<Ty>(a.v, b, 0, h)[n]);
+        const float v = Ty::up(row_of<Ty>(a.v, b, h)[n]);
         float *S = a.state + (size_t)bh * a.Dk * a.Dv + n;
         for (int d = w; d < a.Dk; d += 4) {
             const float s = fmaf(ks[d], v, g * S[(size_t)d * a.Dv]);
