@@ -280,7 +280,7 @@ int deer_layernorm(const deer_norm *n, int64_t rows, const void *x, void *y, flo
 
 size_t deer_layernorm_workspace_bytes(const deer_norm *n, int64_t rows) {
     if (check_norm(n, rows) != DEER_OK) return 0;
-    return layernorm_adjoint_ws_bytes((size_t)rows, n->G, n->D);
+    return layernorm_adjoint_ws_bytes(norm_of(n, rows, nullptr));
 }
 
 int deer_layernorm_adjoint(const deer_norm *n, int64_t rows, const void *x, const void *g, const float *mean,
@@ -296,7 +296,7 @@ int deer_layernorm_adjoint(const deer_norm *n, int64_t rows, const void *x, cons
         set_error("dx, dw and db may not be the same memory");
         return DEER_ERR_INVALID_ARG;
     }
-    if ((rc = check_ws(ws, ws_bytes, layernorm_adjoint_ws_bytes((size_t)rows, n->G, n->D)))) return rc;
+    if ((rc = check_ws(ws, ws_bytes, layernorm_adjoint_ws_bytes(norm_of(n, rows, x))))) return rc;
     return launch_layernorm_adjoint(norm_of(n, rows, x), g, mean, rstd, dx, dw, db, ws, (hipStream_t)stream);
 }
 

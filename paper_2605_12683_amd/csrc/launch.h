@@ -401,7 +401,7 @@ struct NormArgs {
     float eps;
 };
 int launch_layernorm(const NormArgs &a, void *y, float *mean, float *rstd, hipStream_t st);
-size_t layernorm_adjoint_ws_bytes(size_t rows, int G, int D);
+size_t layernorm_adjoint_ws_bytes(const NormArgs &a);
 int launch_layernorm_adjoint(const NormArgs &a, const void *g, const float *mean, const float *rstd, void *dx,
                              float *dw, float *db, void *ws, hipStream_t st);
 

@@ -99,20 +99,6 @@ struct LinRoles {
 typedef uint32_t v2u __attribute__((ext_vector_type(2)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 
-// 16 bytes of a row from element d0 on, zero beyond its width
-template <class Ty>
-__device__ __forceinline__ v4u load_unit(const typename Ty::T *row, int d0, int width, bool vec) {
-    constexpr int E = 16 / sizeof(typename Ty::T);
-    v4u u = {0, 0, 0, 0};
-    if (d0 >= width) return u;
-    if (vec) return *(const v4u *)(row + d0);
-    typename Ty::T x[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = d0 + e < width ? row[d0 + e] : typename Ty::T(0);
-    __builtin_memcpy(&u, x, 16);
-    return u;
-}
-
 // W columns of C rows, NU units of 16 bytes a thread
 template <class Ty, int C, int W>
 struct RowTile {
