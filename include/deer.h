@@ -338,7 +338,7 @@ enum { DEER_F32 = 0, DEER_BF16 = 1, DEER_F16 = 2 };
 
 typedef struct {
     int dtype;          /* DEER_F32, DEER_BF16 or DEER_F16: q, k, v, g, o and the gradients dq, dk, dv */
-    int H;              /* heads of v, o, log_decay and the state                             */
+    int H;              /* heads of v, o, log_decay and the state, 1..16384 (B H up to 2^20)   */
     int Hk;             /* heads of q and k; H % Hk == 0, head h reads head h / (H / Hk)       */
     int Dk, Dv;         /* 1..256 each                                                        */
     int per_step;       /* log_decay: 0 for [H], 1 for [B, T, H] (a step: [B, H])             */
@@ -346,8 +346,8 @@ typedef struct {
 } deer_linattn_shape;
 
 /* An operand [B, T, heads, D] in device memory: element (b, t, h, d) at
- * p + b sb + t st + h sh + d, strides >= 0 in elements (a slice of a fused projection is read
- * in place; any alignment of the elements is allowed). */
+ * p + b sb + t st + h sh + d, strides >= 0 in elements, st at most 2^22 (a slice of a fused
+ * projection is read in place; any alignment of the elements is allowed). */
 typedef struct {
     const void *p;
     int64_t sb, st, sh;

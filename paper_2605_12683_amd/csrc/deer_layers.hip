@@ -12,8 +12,8 @@ static int check_shape(const deer_linattn_shape *s, int B, int T) {
     if (!s) { set_error("shape pointer is NULL"); return DEER_ERR_INVALID_ARG; }
     if (!dtype_ok(s->dtype)) { set_error("unknown dtype %d", s->dtype); return DEER_ERR_INVALID_ARG; }
     if (B <= 0 || T <= 0) { set_error("B and T must be positive (B=%d, T=%d)", B, T); return DEER_ERR_INVALID_ARG; }
-    if (s->H <= 0 || s->Hk <= 0 || s->H % s->Hk != 0) {
-        set_error("H must be a positive multiple of Hk (H=%d, Hk=%d)", s->H, s->Hk);
+    if (s->H <= 0 || s->H > 16384 || s->Hk <= 0 || s->H % s->Hk != 0) {
+        set_error("H must be a multiple of Hk in 1..16384 (H=%d, Hk=%d)", s->H, s->Hk);
         return DEER_ERR_INVALID_ARG;
     }
     if (s->Dk < 1 || s->Dk > 256 || s->Dv < 1 || s->Dv > 256) {
@@ -26,9 +26,13 @@ static int check_shape(const deer_linattn_shape *s, int B, int T) {
     return DEER_OK;
 }
 
-static int check_view(const deer_view *x, const char *name) {
+static int check_view(const deer_view *x, const char *name, int T) {
     if (!x || !x->p) { set_error("%s is required", name); return DEER_ERR_INVALID_ARG; }
     if (x->sb < 0 || x->st < 0 || x->sh < 0) { set_error("the strides of %s must not be negative", name); return DEER_ERR_INVALID_ARG; }
+    if (T > 1 && x->st > (1L << 22)) {
+        set_error("the step stride of %s must not exceed 2^22 elements", name);
+        return DEER_ERR_INVALID_ARG;
+    }
     return DEER_OK;
 }
 
@@ -39,7 +43,9 @@ static int check_alias(const void *out, const char *name, const void *const *in,
     return DEER_OK;
 }
 
-static LinView view_of(const deer_view *x, int r) { return {x->p, (long)x->sb, (long)x->st, (long)x->sh, r}; }
+static LinView view_of(const deer_view *x, int r, int T) {
+    return {x->p, (long)x->sb, T > 1 ? (long)x->st : 0, (long)x->sh, r};
+}
 
 // Segments: enough that the walks' blocks fill the chip twice (two blocks share a CU), none of
 // fewer than kMinSeg steps; one where the walks alone give half of that, since further segments
@@ -47,8 +53,8 @@ static LinView view_of(const deer_view *x, int r) { return {x->p, (long)x->sb, (
 constexpr int kFillBlocks = 512, kMinSeg = 256;
 
 static int segment_steps(const deer_linattn_shape *s, int B, int T, int op) {
-    long blocks = (long)B * s->H * lin_tiles(s->dtype, s->Dk, s->Dv);
-    if (op == DEER_OP_ADJOINT) blocks += 2L * B * s->H * lin_tiles(s->dtype, s->Dv, s->Dk);
+    long blocks = (long)B * s->H * lin_tiles(s->Dk, s->Dv);
+    if (op == DEER_OP_ADJOINT) blocks += 2L * B * s->H * lin_tiles(s->Dv, s->Dk);
     if (2 * blocks >= kFillBlocks || T <= kMinSeg) return T;
     const long n = (kFillBlocks + blocks - 1) / blocks;
     const long steps = ((T + n - 1) / n + 63) / 64 * 64;
@@ -81,7 +87,7 @@ static LinWs carve_lin(void *ws, const deer_linattn_shape *s, int B, int T, int 
             w.dq = c.take<float>(bh * T * s->Dk);
             w.dk = c.take<float>(bh * T * s->Dk);
         }
-        const int tiles = lin_tiles(s->dtype, s->Dv, s->Dk);
+        const int tiles = lin_tiles(s->Dv, s->Dk);
         w.dq_dot = c.take<float>(tiles * bh * T);
         w.dk_dot = c.take<float>(tiles * bh * T);
         w.fwd = c.take<float>(bh * na * s->Dk * s->Dv);
@@ -143,7 +149,7 @@ int deer_linattn(const deer_linattn_shape *s, int B, int T, const deer_view *q, 
     set_error("");
     int rc = check_shape(s, B, T);
     if (rc) return rc;
-    if ((rc = check_view(q, "q")) || (rc = check_view(k, "k")) || (rc = check_view(v, "v"))) return rc;
+    if ((rc = check_view(q, "q", T)) || (rc = check_view(k, "k", T)) || (rc = check_view(v, "v", T))) return rc;
     if (!log_decay || !o) { set_error("log_decay and o are required"); return DEER_ERR_INVALID_ARG; }
     const void *in[] = {q->p, k->p, v->p, log_decay, state0};
     if ((rc = check_alias(o, "o", in, 5)) || (rc = check_alias(state, "state", in, 4))) return rc;
@@ -154,7 +160,7 @@ int deer_linattn(const deer_linattn_shape *s, int B, int T, const deer_view *q, 
     hipStream_t st = (hipStream_t)stream;
     const int r = s->H / s->Hk;
     LinRole ro{};
-    ro.q = view_of(q, r), ro.k = view_of(k, r), ro.v = view_of(v, 1);
+    ro.q = view_of(q, r, T), ro.k = view_of(k, r, T), ro.v = view_of(v, 1, T);
     ro.Kd = s->Dk, ro.N = s->Dv;
     ro.sc_kv = 1.f, ro.sc_o = s->scale;
     ro.out = o, ro.wide_out = wide_out(o, s->dtype, s->Dv);
@@ -174,7 +180,8 @@ int deer_linattn_adjoint(const deer_linattn_shape *s, int B, int T, const deer_v
     set_error("");
     int rc = check_shape(s, B, T);
     if (rc) return rc;
-    if ((rc = check_view(q, "q")) || (rc = check_view(k, "k")) || (rc = check_view(v, "v")) || (rc = check_view(g, "g")))
+    if ((rc = check_view(q, "q", T)) || (rc = check_view(k, "k", T)) || (rc = check_view(v, "v", T)) ||
+        (rc = check_view(g, "g", T)))
         return rc;
     if (!log_decay || !dq || !dk || !dv) { set_error("log_decay, dq, dk and dv are required"); return DEER_ERR_INVALID_ARG; }
     const void *in[] = {q->p, k->p, v->p, g->p, log_decay, state0, g_state};
@@ -189,7 +196,7 @@ int deer_linattn_adjoint(const deer_linattn_shape *s, int B, int T, const deer_v
     const LinWs w = carve_lin(ws, s, B, T, DEER_OP_ADJOINT);
     const int r = s->H / s->Hk, Dk = s->Dk, Dv = s->Dv;
     const bool shared = r > 1, decay = dlog_decay != nullptr;
-    const LinView vq = view_of(q, r), vk = view_of(k, r), vv = view_of(v, 1), vg = view_of(g, 1);
+    const LinView vq = view_of(q, r, T), vk = view_of(k, r, T), vv = view_of(v, 1, T), vg = view_of(g, 1, T);
     LinRole ro[3] = {};
     // dq: the state is S^T [Dv, Dk]
     ro[0].q = vg, ro[0].k = vv, ro[0].v = vk;
@@ -216,7 +223,7 @@ int deer_linattn_adjoint(const deer_linattn_shape *s, int B, int T, const deer_v
     ro[2].fin = dstate0, ro[2].fin_d = Dv, ro[2].fin_n = 1;
     const LinArgs a = args_of(s, B, T, DEER_OP_ADJOINT, log_decay, lengths);
     hipStream_t st = (hipStream_t)stream;
-    const bool same = lin_same_tile(s->dtype, Dv, Dk, Dk, Dv);
+    const bool same = lin_same_tile(Dv, Dk, Dk, Dv);
     if (a.nseg > 1) {
         ro[0].seg = w.seg, ro[0].seg_decay = w.seg_decay, ro[0].seg_d = Dk, ro[0].seg_n = 1;
         ro[2].seg = w.rseg, ro[2].seg_decay = w.rseg_decay, ro[2].seg_d = Dv, ro[2].seg_n = 1;
@@ -242,7 +249,7 @@ int deer_linattn_adjoint(const deer_linattn_shape *s, int B, int T, const deer_v
         if ((rc = launch_lin_head_sum(s->dtype, rows, s->Hk, r, Dk, w.dk, dk, st))) return rc;
     }
     if (!decay) return DEER_OK;
-    const int tiles = lin_tiles(s->dtype, Dv, Dk);
+    const int tiles = lin_tiles(Dv, Dk);
     return launch_lin_decay_grad(a, w.dq_dot, tiles, w.dk_dot, tiles, w.fwd, w.rev, Dk * Dv, w.part, dlog_decay, st);
 }
 
@@ -251,14 +258,14 @@ int deer_linattn_step(const deer_linattn_shape *s, int B, const deer_view *q, co
     set_error("");
     int rc = check_shape(s, B, 1);
     if (rc) return rc;
-    if ((rc = check_view(q, "q")) || (rc = check_view(k, "k")) || (rc = check_view(v, "v"))) return rc;
+    if ((rc = check_view(q, "q", 1)) || (rc = check_view(k, "k", 1)) || (rc = check_view(v, "v", 1))) return rc;
     if (!log_decay || !state || !o) { set_error("log_decay, state and o are required"); return DEER_ERR_INVALID_ARG; }
     const void *in[] = {q->p, k->p, v->p, log_decay};
     if ((rc = check_alias(o, "o", in, 4)) || (rc = check_alias(state, "state", in, 4))) return rc;
     if ((void *)state == o) { set_error("o and state may not be the same memory"); return DEER_ERR_INVALID_ARG; }
     const int r = s->H / s->Hk;
-    LinStep a{s->dtype, B, s->H, s->Hk, s->Dk, s->Dv, s->per_step != 0, s->scale, view_of(q, r), view_of(k, r),
-              view_of(v, 1), log_decay, lengths, state, o};
+    LinStep a{s->dtype, B, s->H, s->Hk, s->Dk, s->Dv, s->per_step != 0, s->scale, view_of(q, r, 1), view_of(k, r, 1),
+              view_of(v, 1, 1), log_decay, lengths, state, o};
     return launch_lin_step(a, (hipStream_t)stream);
 }
 

@@ -64,22 +64,19 @@ int launch_lin_join(const LinArgs &a, const LinRole *roles, int nroles, hipStrea
     return DEER_OK;
 }
 
-static int parts_of(int dtype) { return dtype == DEER_F32 ? 3 : dtype == DEER_F16 ? 2 : 1; }
-
-int lin_tiles(int dtype, int Kd, int N) {
-    const int nb = 4 * cw_of(parts_of(dtype), kt_of(Kd), N);
+int lin_tiles(int Kd, int N) {
+    const int nb = 16 * nw_of(kt_of(Kd), N);
     return (N + nb - 1) / nb;
 }
 
-bool lin_same_tile(int dtype, int Kd, int N, int Kd2, int N2) {
-    const int p = parts_of(dtype);
-    return kt_of(Kd) == kt_of(Kd2) && cw_of(p, kt_of(Kd), N) == cw_of(p, kt_of(Kd2), N2);
+bool lin_same_tile(int Kd, int N, int Kd2, int N2) {
+    return kt_of(Kd) == kt_of(Kd2) && nw_of(kt_of(Kd), N) == nw_of(kt_of(Kd2), N2);
 }
 
-int launch_lin_walk(const LinArgs &a, const LinRole *roles, int nroles, bool states, bool fine, hipStream_t st) {
-    if (a.dtype == DEER_F32) return launch_lin_walk_f32(a, roles, nroles, states, fine, st);
-    if (a.dtype == DEER_BF16) return launch_lin_walk_bf16(a, roles, nroles, states, fine, st);
-    return launch_lin_walk_f16(a, roles, nroles, states, fine, st);
+int launch_lin_walk(const LinArgs &a, const LinRole *roles, int nroles, bool states, bool dots, hipStream_t st) {
+    if (a.dtype == DEER_F32) return launch_lin_walk_f32(a, roles, nroles, states, dots, st);
+    if (a.dtype == DEER_BF16) return launch_lin_walk_bf16(a, roles, nroles, states, dots, st);
+    return launch_lin_walk_f16(a, roles, nroles, states, dots, st);
 }
 
 // ---- the gradient of the log decays --------------------------------------------------------------

@@ -3,8 +3,9 @@
 
 namespace deer {
 
-int launch_lin_walk_f32(const LinArgs &a, const LinRole *roles, int n, bool states, bool fine, hipStream_t st) {
-    return states ? launch_walk_parts<F32, 3, false>(a, roles, n, st) : launch_walk_parts<F32, 3, true>(a, roles, n, st);
+int launch_lin_walk_f32(const LinArgs &a, const LinRole *roles, int n, bool states, bool dots, hipStream_t st) {
+    if (states) return launch_walk_parts<F32, 3, kStates>(a, roles, n, st);
+    return dots ? launch_walk_parts<F32, 3, kOutDots>(a, roles, n, st) : launch_walk_parts<F32, 3, kOut>(a, roles, n, st);
 }
 
 }  // namespace deer

@@ -363,16 +363,17 @@ struct LinArgs {
     const int32_t *lengths;     // [B] or null
     int seg_steps, nseg;        // segments of seg_steps steps (a multiple of 64), or one of all T
 };
-int lin_tiles(int dtype, int Kd, int N);   // blocks that share the N columns of one head's state
-bool lin_same_tile(int dtype, int Kd, int N, int Kd2, int N2);
+int lin_tiles(int Kd, int N);   // blocks that share the N columns of one head's state
+bool lin_same_tile(int Kd, int N, int Kd2, int N2);
 // all roles of one call have the same tile shape; states: what each segment adds (into seg,
-// seg_decay), else the outputs; fine: intermediate values of 16-bit operands in 24 bits, not 16
-int launch_lin_walk(const LinArgs &a, const LinRole *roles, int nroles, bool states, bool fine, hipStream_t st);
+// seg_decay), else the outputs; dots: and dot, anchor (which are summed over many steps, so the
+// intermediate values of 16-bit operands then take 24 bits, not 16)
+int launch_lin_walk(const LinArgs &a, const LinRole *roles, int nroles, bool states, bool dots, hipStream_t st);
 // seg from what each segment adds to the state entering it; fin
 int launch_lin_join(const LinArgs &a, const LinRole *roles, int nroles, hipStream_t st);
-int launch_lin_walk_bf16(const LinArgs &a, const LinRole *roles, int n, bool states, bool fine, hipStream_t st);
-int launch_lin_walk_f16(const LinArgs &a, const LinRole *roles, int n, bool states, bool fine, hipStream_t st);
-int launch_lin_walk_f32(const LinArgs &a, const LinRole *roles, int n, bool states, bool fine, hipStream_t st);
+int launch_lin_walk_bf16(const LinArgs &a, const LinRole *roles, int n, bool states, bool dots, hipStream_t st);
+int launch_lin_walk_f16(const LinArgs &a, const LinRole *roles, int n, bool states, bool dots, hipStream_t st);
+int launch_lin_walk_f32(const LinArgs &a, const LinRole *roles, int n, bool states, bool dots, hipStream_t st);
 // gradient of the log decays from the dots of dq and dk and the states at the anchors:
 // part is [B, H, anchors] doubles
 int launch_lin_decay_grad(const LinArgs &a, const float *dq_dot, int q_tiles, const float *dk_dot, int k_tiles,

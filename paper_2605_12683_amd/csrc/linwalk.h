@@ -14,8 +14,8 @@
 // bits, for 16-bit outputs, 2^8 times finer than their own rounding; three: float32's 24) and always
 // into three where it enters the state, which is float32 for as long as the sequence lasts.
 //
-// One block of four waves walks one head's chunks for NB = 4 CW columns of the state; a wave keeps
-// its CW columns in registers for the whole walk, as matrix-core accumulators.  Their lane layout
+// One block of NW waves walks one head's chunks for 16 NW columns of the state; a wave keeps its 16
+// columns in registers for the whole walk, as matrix-core accumulators.  Their lane layout
 // (rows 4 g + r, column c of lane 16 g + c) is also that of an operand with the rows as the summed
 // index, if the other operand lists them in the order 4 g + 0..3, 16 + 4 g + 0..3 of each 32: q is
 // stored in LDS in that order, and the state enters its product with no exchange between lanes.  k
@@ -71,23 +71,29 @@ struct InParts<F16> { static constexpr int n = 2; };
 template <>
 struct InParts<F32> { static constexpr int n = 3; };
 
-// padded width of the summed side, and columns per wave: 32 where the state then fits the registers
-// (Kd <= 128) and the columns fill more than half a block; 16 with float32 tiles of 128, whose LDS
-// tiles would leave one block to a CU
+// padded width of the summed side, and waves of 16 columns per block: eight where the columns fill
+// more than half of them and the state leaves the registers for four waves a SIMD (Kd <= 128)
 constexpr int kt_of(int Kd) { return Kd <= 32 ? 32 : Kd <= 64 ? 64 : Kd <= 128 ? 128 : 256; }
-constexpr int cw_of(int parts, int KT, int N) { return N > 64 && KT <= (parts == 3 ? 64 : 128) ? 32 : 16; }
+constexpr int nw_of(int KT, int N) { return N > 64 && KT <= 128 ? 8 : 4; }
 
-template <int NPI, int KT, int CW, int NPX, bool OUT>
+// what a walk leaves: the state that each segment adds by itself, from zero, and its decay; the
+// outputs (and the last state) from the state entering each segment; and with them the dots and the
+// states at the anchors
+enum { kStates = 0, kOut = 1, kOutDots = 2 };
+
+template <int NPI, int KT, int NW, int NPX, int MODE>
 struct LinTile {
-    static constexpr int NB = 4 * CW;
+    static constexpr bool OUT = MODE != kStates;
+    static constexpr int NB = 16 * NW, TH = 64 * NW;
     static constexpr int PQ = KT + 8, PK = KT + 16, PV = NB + 16;   // LDS row pitches: no bank conflicts
-    static constexpr int bytes(int C) {
+    static constexpr int bytes(int C) {   // (the dots lie where q was)
         return NPI * C * 2 * ((OUT ? PQ : 0) + PK + PV) + (OUT ? (C / 16) * (C / 32) * NPX * 1024 : 0) +
-               2 * (4 * C + 4) * 4 + 4 * C * 4;
+               2 * (4 * C + 4) * 4;
     }
     static constexpr int C = bytes(64) <= 80 * 1024 ? 64 : 32;
     static constexpr int lds = bytes(C);
-    static constexpr int waves = lds <= 80 * 1024 ? 2 : 1;          // per SIMD
+    static constexpr int fit = 160 * 1024 / lds * NW / 4;
+    static constexpr int waves = fit > 4 ? 4 : fit;                 // per SIMD
 };
 
 struct LinRoles {
@@ -99,20 +105,66 @@ struct LinRoles {
 typedef uint32_t v2u __attribute__((ext_vector_type(2)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 
-// W columns of C rows, NU units of 16 bytes a thread
-template <class Ty, int C, int W>
+// x again, as a value that the compiler does not know to be the same: what is computed from it stays
+// where it is written, instead of living in registers across the walk's loop
+__device__ __forceinline__ int afresh(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+// offsets of 2^31 or more lie outside every resource used here: loads give zero, stores are dropped
+constexpr uint32_t kOutside = 0x80000000u;
+
+// One operand's rows of one (sequence, head): W columns from col0 on, C rows a chunk, NU units of 16
+// bytes a thread.  A chunk is read as a bounded buffer, whose 32-bit offsets (C st stays below 2^31
+// bytes by the limit on st) are the same for every chunk: by units where rows start on 16 bytes and
+// do not overlap, rows behind the sequence's end then lying outside; else by elements.
+template <class Ty, int C, int W, int TH>
 struct RowTile {
-    static constexpr int E = 16 / sizeof(typename Ty::T), UPR = W / E, NU = (C * UPR + 255) / 256;
+    using T = typename Ty::T;
+    static constexpr int E = 16 / sizeof(T), UPR = W / E, NU = (C * UPR + TH - 1) / TH, ROWS = TH / UPR;
+    const T *base;
+    int st, width, step, d;        // st, step in bytes
+    uint32_t off;
+    bool fast, rev;
     v4u u[NU];
 
-    __device__ __forceinline__ void load(const typename Ty::T *base, long st, int t0, bool rev, int len, int col0,
-                                         int width, bool vec) {
+    __device__ __forceinline__ void init(const LinView &x, int b, int h, int col0, int width_, bool rev_) {
+        base = (const T *)x.p + b * x.sb + (h / x.r) * x.sh;
+        st = (int)(x.st * (long)sizeof(T)), width = width_, rev = rev_;
+        fast = (((uintptr_t)base | (uintptr_t)st) & 15) == 0 && width % E == 0 && x.st >= width;
+        const int row = threadIdx.x / UPR;
+        d = col0 + (threadIdx.x % UPR) * E;
+        step = rev ? -ROWS * st : ROWS * st;
+        off = d < width && row < C ? (uint32_t)((rev ? C - 1 - row : row) * st + d * (int)sizeof(T)) : kOutside;
+    }
+
+    __device__ __forceinline__ void load(int t0, int len) {
+        const int rows = len - t0 < C ? len - t0 : C;
+        const auto rs = bounded_rsrc((const char *)base + (long)t0 * st,
+                                     rows > 0 ? (uint32_t)((rows - 1) * st + width * (int)sizeof(T)) : 0u);
+        const uint32_t o = (uint32_t)afresh((int)off);
+        if (fast) {
+#pragma unroll
+            for (int i = 0; i < NU; ++i)
+                u[i] = __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)(o + (uint32_t)(i * step)), 0, 0));
+            return;
+        }
+        const int r0 = afresh((int)(threadIdx.x / UPR));
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
-            const int n = i * 256 + threadIdx.x, row = n / UPR, d = (n % UPR) * E;
-            const int t = rev ? t0 + C - 1 - row : t0 + row;
-            u[i] = v4u{0, 0, 0, 0};
-            if ((C * UPR % 256 == 0 || row < C) && t < len) u[i] = load_unit<Ty>(base + t * st, col0 + d, width, vec);
+            const int row = i * ROWS + r0, j = rev ? C - 1 - row : row;
+            const bool on = row < C && j < rows;
+            uint32_t x[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const int at = on && d + e < width ? (int)(o + (uint32_t)(i * step) + e * sizeof(T)) : (int)kOutside;
+                if constexpr (sizeof(T) == 4) x[e] = bload_u(rs, (uint32_t)at, 0);
+                else x[e] = __builtin_bit_cast(uint16_t, __builtin_amdgcn_raw_buffer_load_b16(rs, at, 0, 0));
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) u[i][k] = sizeof(T) == 4 ? x[k] : x[2 * k] | x[2 * k + 1] << 16;
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
 
@@ -122,8 +174,8 @@ struct RowTile {
         constexpr int NP = InParts<Ty>::n;
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
-            const int n = i * 256 + threadIdx.x, row = n / UPR, d = (n % UPR) * E;
-            if (C * UPR % 256 != 0 && row >= C) continue;
+            const int n = i * TH + threadIdx.x, row = n / UPR, d = (n % UPR) * E;
+            if (C * UPR % TH != 0 && row >= C) continue;
 #pragma unroll
             for (int half = 0; half < E / 4; ++half) {   // four elements at a time
                 uint32_t p[NP][2];
@@ -210,17 +262,30 @@ struct Decays {
     float pad[3];
 };
 
-// by one wave; raw: this lane's log decay (lanes beyond C repeat the others).  Returns L.
+// the double that the DPP control CTRL brings from another lane, 0 where it brings none
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp_or_zero(double x) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t l = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, ROWS, 15, false);
+    const uint32_t h = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, ROWS, 15, false);
+    return __builtin_bit_cast(double, ((uint64_t)h << 32) | l);
+}
+
+// by one wave; raw: this lane's log decay (C = 32: the upper half wave repeats the lower).  Returns L.
 template <int C>
 __device__ __forceinline__ double chunk_decays(Decays<C> &d, float raw, float sc_kv) {
     const int lane = threadIdx.x & 63, i = lane & (C - 1);
     double s = gate_of(raw);
-#pragma unroll
-    for (int off = 1; off < C; off <<= 1) {
-        const double o = __shfl_up(s, off, C);
-        if (i >= off) s += o;
-    }
-    const double L = __shfl(s, C - 1, C);
+    s += dpp_or_zero<0x111, 15>(s);        // row_shr: lanes of each 16
+    s += dpp_or_zero<0x112, 15>(s);
+    s += dpp_or_zero<0x114, 15>(s);
+    s += dpp_or_zero<0x118, 15>(s);
+    s += dpp_or_zero<0x142, 0xa>(s);       // row_bcast:15 into rows 1 and 3
+    if (C == 64) s += dpp_or_zero<0x143, 0xc>(s);   // row_bcast:31 into rows 2 and 3
+    const uint64_t u = __builtin_bit_cast(uint64_t, s);
+    const double L = __builtin_bit_cast(
+        double, ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), C - 1) << 32) |
+                    (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, C - 1));
     const float hi = (float)s;
     d.hi[i] = hi;
     d.lo[i] = (float)(s - (double)hi);
@@ -232,22 +297,21 @@ __device__ __forceinline__ double chunk_decays(Decays<C> &d, float raw, float sc
 
 // ---- the walk ---------------------------------------------------------------------------------
 
-// OUT: outputs (and the last state, dots, anchors) of each segment from the state entering it;
-// otherwise the state that each segment adds by itself, from zero, and its decay.
-template <class Ty, int KT, int CW, int NPX, bool OUT>
-__global__ __launch_bounds__(256, (LinTile<InParts<Ty>::n, KT, CW, NPX, OUT>::waves)) void k_lin_walk(LinArgs a,
-                                                                                                     LinRoles rs) {
+template <class Ty, int KT, int NW, int NPX, int MODE>
+__global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, NPX, MODE>::waves)) void k_lin_walk(LinArgs a,
+                                                                                                          LinRoles rs) {
     constexpr int NPI = InParts<Ty>::n;
-    using Tile = LinTile<NPI, KT, CW, NPX, OUT>;
+    using Tile = LinTile<NPI, KT, NW, NPX, MODE>;
     using T = typename Ty::T;
-    constexpr int C = Tile::C, NB = Tile::NB, PQ = Tile::PQ, PK = Tile::PK, PV = Tile::PV;
-    constexpr int NT = C / 16, KS = C / 32, DT = KT / 16, CT = CW / 16;
+    constexpr bool OUT = Tile::OUT, DOTS = MODE == kOutDots;
+    constexpr int C = Tile::C, NB = Tile::NB, TH = Tile::TH, PQ = Tile::PQ, PK = Tile::PK, PV = Tile::PV;
+    constexpr int NT = C / 16, KS = C / 32, DT = KT / 16;
     extern __shared__ __align__(16) unsigned char smem[];
     uint16_t *Ks = (uint16_t *)smem, *Vs = Ks + NPI * C * PK, *Qs = Vs + NPI * C * PV;
     unsigned char *rest = (unsigned char *)(Qs + (OUT ? NPI * C * PQ : 0));
     v4u *Ps = (v4u *)rest;                                     // [NT][KS][NPX][64 lanes]
     Decays<C> *dec = (Decays<C> *)(rest + (OUT ? NT * KS * NPX * 1024 : 0));
-    float *dots = (float *)(dec + 2);                          // [4][C]
+    float *dots = (float *)Qs;                                 // [NW][C], between the chunk's last two barriers
 
     const LinRole &ro = rs.r[blockIdx.y];
     const int tiles = (ro.N + NB - 1) / NB;
@@ -260,27 +324,24 @@ __global__ __launch_bounds__(256, (LinTile<InParts<Ty>::n, KT, CW, NPX, OUT>::wa
     const int len = length_of(a, b);
     const int lo = seg * a.seg_steps, hi = lo + a.seg_steps < a.T ? lo + a.seg_steps : a.T;
     const int chunks = (hi - lo + C - 1) / C;
-    const size_t mat = (size_t)ro.Kd * ro.N;
-    const int col0 = tile * NB, n0 = col0 + w * CW;            // the block's and the wave's first column
+    const int Kd = ro.Kd, N = ro.N;
+    const size_t mat = (size_t)Kd * N;
+    const int col0 = tile * NB, n0 = col0 + w * 16;            // the block's and the wave's first column
 
     // the segment that comes last adds to no other: its own sum is needed for the last state only
     if (!OUT && seg == (rev ? 0 : a.nseg - 1) && !ro.fin) return;
 
-    const T *qb = (const T *)ro.q.p + b * ro.q.sb + (h / ro.q.r) * ro.q.sh;
-    const T *kb = (const T *)ro.k.p + b * ro.k.sb + (h / ro.k.r) * ro.k.sh;
-    const T *vb = (const T *)ro.v.p + b * ro.v.sb + (h / ro.v.r) * ro.v.sh;
-    constexpr int E = 16 / sizeof(T);
-    auto wide = [](const T *p, long st, int n) { return (((uintptr_t)p | (uintptr_t)(st * sizeof(T))) & 15) == 0 && n % E == 0; };
-    const bool qw = OUT && wide(qb, ro.q.st, ro.Kd), kw = wide(kb, ro.k.st, ro.Kd), vw = wide(vb, ro.v.st, ro.N);
-
-    RowTile<Ty, C, KT> qr, kr;
-    RowTile<Ty, C, NB> vr;
+    RowTile<Ty, C, KT, TH> qr, kr;
+    RowTile<Ty, C, NB, TH> vr;
+    kr.init(ro.k, b, h, 0, Kd, rev);
+    vr.init(ro.v, b, h, col0, N, rev);
+    if constexpr (OUT) qr.init(ro.q, b, h, 0, Kd, rev);
     auto t0_of = [&](int n) { return lo + (rev ? chunks - 1 - n : n) * C; };
     auto load = [&](int n) {
         const int t0 = t0_of(n);
-        kr.load(kb, ro.k.st, t0, rev, len, 0, ro.Kd, kw);
-        vr.load(vb, ro.v.st, t0, rev, len, col0, ro.N, vw);
-        if constexpr (OUT) qr.load(qb, ro.q.st, t0, rev, len, 0, ro.Kd, qw);
+        kr.load(t0, len);
+        vr.load(t0, len);
+        if constexpr (OUT) qr.load(t0, len);
     };
     auto gate = [&](int n) {
         if (n >= chunks) return 0.f;
@@ -288,7 +349,12 @@ __global__ __launch_bounds__(256, (LinTile<InParts<Ty>::n, KT, CW, NPX, OUT>::wa
         return gate_raw(a, b, h, t0_of(n) + (rev ? C - 1 - i : i), len, rev);
     };
 
-    v4f S[DT][CT];
+    // element (d, n) of a matrix of Kd N floats, beyond its rows and columns outside
+    v4f S[DT];
+    auto at = [&](int l, int dt, int r, int sd, int sn) {
+        const int d = dt * 16 + 4 * (l >> 4) + r, n = n0 + (l & 15);
+        return d < Kd && n < N ? (uint32_t)(d * sd + n * sn) * 4u : kOutside;
+    };
     {
         const float *src = nullptr;
         int sd = 0, sn = 0;
@@ -296,35 +362,46 @@ __global__ __launch_bounds__(256, (LinTile<InParts<Ty>::n, KT, CW, NPX, OUT>::wa
             if (a.nseg > 1) src = ro.seg + ((size_t)bh * a.nseg + seg) * mat, sd = ro.seg_d, sn = ro.seg_n;
             else if (ro.init) src = ro.init + bh * mat, sd = ro.init_d, sn = ro.init_n;
         }
+        const auto rsrc = bounded_rsrc(src, src ? (uint32_t)(mat * 4) : 0u);
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int d = dt * 16 + 4 * g + r, n = n0 + ct * 16 + c;
-                    S[dt][ct][r] = src && d < ro.Kd && n < ro.N ? src[(size_t)d * sd + (size_t)n * sn] : 0.f;
-                }
+                for (int r = 0; r < 4; ++r) S[dt][r] = bload(rsrc, at(lane, dt, r, sd, sn), 0);
     }
     auto put_state = [&](float *dst, int sd, int sn, float f) {
+        const auto rsrc = bounded_rsrc(dst, (uint32_t)(mat * 4));
+        const int l = afresh(lane);
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int d = dt * 16 + 4 * g + r, n = n0 + ct * 16 + c;
-                    if (d < ro.Kd && n < ro.N) dst[(size_t)d * sd + (size_t)n * sn] = f * S[dt][ct][r];
+                    bstore_u(rsrc, __float_as_uint(f * S[dt][r]), at(l, dt, r, sd, sn), 0);
+                    if (r == 3) __builtin_amdgcn_sched_barrier(0);
                 }
     };
 
+    // this lane's part of the outputs: step i = 16 it + c of a chunk, columns n0 + 4 g + 0..3
+    const int out_size = ro.out_f32 ? 4 : (int)sizeof(T), out_row = a.H * N * out_size;   // C rows below 2^31 bytes
+    auto out_off = [&](int l, int it, int row, int size) {
+        const int i = it * 16 + (l & 15), n = n0 + 4 * (l >> 4);
+        return n < N ? (uint32_t)((rev ? C - 1 - i : i) * row + n * size) : kOutside;
+    };
+    const T *partner = nullptr;
+    bool partner_fast = false;
+    if constexpr (DOTS) {
+        partner = (const T *)ro.partner.p + b * ro.partner.sb + (h / ro.partner.r) * ro.partner.sh;
+        const long row = ro.partner.st * (long)sizeof(T);
+        partner_fast = (((uintptr_t)partner | (uintptr_t)row) & (4 * sizeof(T) - 1)) == 0 && N % 4 == 0 &&
+                       ro.partner.st >= N;
+    }
+
     // tiles above the diagonal that share an operand with one on it stay zero
     if constexpr (OUT)
-        for (int i = threadIdx.x; i < NT * KS * NPX * 64; i += 256) Ps[i] = v4u{0, 0, 0, 0};
+        for (int i = threadIdx.x; i < NT * KS * NPX * 64; i += TH) Ps[i] = v4u{0, 0, 0, 0};
     load(0);
-    double total = 0.0;                                        // wave 3: log2 decay of the segment
+    double total = 0.0;                                        // last wave: log2 decay of the segment
     float raw = 0.f;
-    if (w == 3) {
+    if (w == NW - 1) {
         total += chunk_decays<C>(dec[0], gate(0), ro.sc_kv);
         raw = gate(1);
     }
@@ -339,20 +416,22 @@ __global__ __launch_bounds__(256, (LinTile<InParts<Ty>::n, KT, CW, NPX, OUT>::wa
         lds_barrier();
         if (n + 1 < chunks) {
             load(n + 1);
-            if (w == 3) {
+            if (w == NW - 1) {
                 total += chunk_decays<C>(dec[(n + 1) & 1], raw, ro.sc_kv);
                 raw = gate(n + 2);
             }
         }
         float *anc = nullptr;
-        if (OUT && ro.anchor && ((t0 + C) % kLinAnchor == 0 || t0 + C >= a.T))
-            anc = ro.anchor + ((size_t)bh * na + t0 / kLinAnchor) * mat;
-        if (OUT && anc && rev) put_state(anc, ro.N, 1, 1.f);
+        if constexpr (DOTS) {
+            if ((t0 + C) % kLinAnchor == 0 || t0 + C >= a.T) anc = ro.anchor + ((size_t)bh * na + t0 / kLinAnchor) * mat;
+            if (anc && rev) put_state(anc, N, 1, 1.f);
+        }
+        __builtin_amdgcn_sched_barrier(0);
 
-        v4f O[NT][CT];
+        v4f O[NT];
         if constexpr (OUT) {
             // decayed scores, transposed: rows j, columns i
-            for (int tl = w; tl < NT * (NT + 1) / 2; tl += 4) {
+            for (int tl = w; tl < NT * (NT + 1) / 2; tl += NW) {
                 const int it = tl >= 6 ? 3 : tl >= 3 ? 2 : tl >= 1 ? 1 : 0, jt = tl - it * (it + 1) / 2;
                 v4f acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -385,78 +464,94 @@ __global__ __launch_bounds__(256, (LinTile<InParts<Ty>::n, KT, CW, NPX, OUT>::wa
             }
             // what the entering state gives, transposed: rows n, columns i
 #pragma unroll
-            for (int it = 0; it < NT; ++it)
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct) O[it][ct] = v4f{0.f, 0.f, 0.f, 0.f};
+            for (int it = 0; it < NT; ++it) O[it] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int u = 0; u < KT / 32; ++u) {
-                v4u sf[CT][NPX];
+                v4u sf[NPX];
+                float x[8];
 #pragma unroll
-                for (int ct = 0; ct < CT; ++ct) {
-                    float x[8];
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) x[r] = S[2 * u][ct][r], x[4 + r] = S[2 * u + 1][ct][r];
-                    split8<NPX>(x, sf[ct]);
-                }
+                for (int r = 0; r < 4; ++r) x[r] = S[2 * u][r], x[4 + r] = S[2 * u + 1][r];
+                split8<NPX>(x, sf);
 #pragma unroll
                 for (int it = 0; it < NT; ++it) {
                     v4u qf[NPI];
 #pragma unroll
                     for (int p = 0; p < NPI; ++p) qf[p] = *(const v4u *)(Qs + (p * C + it * 16 + c) * PQ + u * 32 + 8 * g);
-#pragma unroll
-                    for (int ct = 0; ct < CT; ++ct) O[it][ct] = mfma_parts<NPX - 1>(sf[ct], qf, O[it][ct]);
+                    O[it] = mfma_parts<NPX - 1>(sf, qf, O[it]);
                 }
+                __builtin_amdgcn_sched_barrier(0);   // (parts of one 32 rows of the state at a time)
             }
+#pragma unroll
+            for (int it = 0; it < NT; ++it) O[it] *= dc.from[it * 16 + c];
+            lds_barrier();
+        }
+
+        // the partner's rows, used at the end
+        typedef T v4t __attribute__((ext_vector_type(4)));
+        v4t pr[DOTS ? NT : 1];
+        if constexpr (DOTS) {
+            const int rows = len - t0 < C ? len - t0 : C;
+            const auto prs = bounded_rsrc(partner + t0 * ro.partner.st,
+                                          rows > 0 ? (uint32_t)(((rows - 1) * ro.partner.st + N) * sizeof(T)) : 0u);
+            const int row = (int)(ro.partner.st * (long)sizeof(T)), l = afresh(lane);
 #pragma unroll
             for (int it = 0; it < NT; ++it) {
-                const float f = dc.from[it * 16 + c];
+                const int off = (int)out_off(l, it, row, sizeof(T));
+                if (partner_fast) {
+                    if constexpr (sizeof(T) == 4)
+                        pr[it] = __builtin_bit_cast(v4t, __builtin_amdgcn_raw_buffer_load_b128(prs, off, 0, 0));
+                    else
+                        pr[it] = __builtin_bit_cast(v4t, __builtin_amdgcn_raw_buffer_load_b64(prs, off, 0, 0));
+                    continue;
+                }
+                const int i = it * 16 + (l & 15), j = rev ? C - 1 - i : i, nn = n0 + 4 * (l >> 4);
 #pragma unroll
-                for (int ct = 0; ct < CT; ++ct) O[it][ct] *= f;
+                for (int r = 0; r < 4; ++r) {
+                    const int at = j < rows && nn + r < N ? off + r * (int)sizeof(T) : (int)kOutside;
+                    if constexpr (sizeof(T) == 4)
+                        pr[it][r] = bload(prs, (uint32_t)at, 0);
+                    else
+                        pr[it][r] = __builtin_bit_cast(T, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(prs, at, 0, 0));
+                }
             }
-            lds_barrier();
         }
 
         // the chunk's own steps, and the state at its end
         const float all = dc.all;
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) S[dt][ct] *= all;
+        for (int dt = 0; dt < DT; ++dt) S[dt] *= all;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-            v4u vf[CT][NPI], sv[CT][3];
+            v4u vf[NPI], sv[3];
+            float x[8];
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct) {
-                float x[8];
+            for (int e = 0; e < 8; ++e) x[e] = 0.f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = 0.f;
+            for (int p = 0; p < NPI; ++p) {
+                const uint16_t *vp = Vs + p * C * PV;
+                const v2u v0 = read_turned(vp, PV, ks * 32, w * 16, g, c);
+                const v2u v1 = read_turned(vp, PV, ks * 32 + 16, w * 16, g, c);
+                vf[p] = v4u{v0[0], v0[1], v1[0], v1[1]};
 #pragma unroll
-                for (int p = 0; p < NPI; ++p) {
-                    const uint16_t *vp = Vs + p * C * PV;
-                    const v2u v0 = read_turned(vp, PV, ks * 32, w * CW + ct * 16, g, c);
-                    const v2u v1 = read_turned(vp, PV, ks * 32 + 16, w * CW + ct * 16, g, c);
-                    vf[ct][p] = v4u{v0[0], v0[1], v1[0], v1[1]};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        x[2 * e] += __uint_as_float(vf[ct][p][e] << 16);
-                        x[2 * e + 1] += __uint_as_float(vf[ct][p][e] & 0xffff0000u);
-                    }
+                for (int e = 0; e < 4; ++e) {
+                    x[2 * e] += __uint_as_float(vf[p][e] << 16);
+                    x[2 * e + 1] += __uint_as_float(vf[p][e] & 0xffff0000u);
                 }
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    x[r] *= dc.into[ks * 32 + 4 * g + r];
-                    x[4 + r] *= dc.into[ks * 32 + 16 + 4 * g + r];
-                }
-                split8<3>(x, sv[ct]);
             }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                x[r] *= dc.into[ks * 32 + 4 * g + r];
+                x[4 + r] *= dc.into[ks * 32 + 16 + 4 * g + r];
+            }
+            split8<3>(x, sv);
+            __builtin_amdgcn_sched_barrier(0);
             if constexpr (OUT) {
 #pragma unroll
                 for (int it = 2 * ks; it < NT; ++it) {
                     v4u pf[NPX];
 #pragma unroll
                     for (int q = 0; q < NPX; ++q) pf[q] = Ps[((it * KS + ks) * NPX + q) * 64 + lane];
-#pragma unroll
-                    for (int ct = 0; ct < CT; ++ct) O[it][ct] = mfma_parts<NPX - 1>(vf[ct], pf, O[it][ct]);
+                    O[it] = mfma_parts<NPX - 1>(vf, pf, O[it]);
                 }
             }
 #pragma unroll
@@ -469,61 +564,68 @@ __global__ __launch_bounds__(256, (LinTile<InParts<Ty>::n, KT, CW, NPX, OUT>::wa
                     const v2u k1 = read_turned(kp, PK, ks * 32 + 16, dt * 16, g, c);
                     kf[p] = v4u{k0[0], k0[1], k1[0], k1[1]};
                 }
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct) S[dt][ct] = mfma_parts<2>(kf, sv[ct], S[dt][ct]);
+                S[dt] = mfma_parts<2>(kf, sv, S[dt]);
+                if (dt % 4 == 3) __builtin_amdgcn_sched_barrier(0);
             }
         }
 
+        __builtin_amdgcn_sched_barrier(0);
         if constexpr (OUT) {
+            const bool tail = t0 + C > len;      // some rows lie behind the sequence's end: zero
 #pragma unroll
             for (int it = 0; it < NT; ++it) {
-                const int i = it * 16 + c, t = rev ? t0 + C - 1 - i : t0 + i;
-                const bool live = t < len;
-                float dot = 0.f;
+                const int i = it * 16 + c, j = rev ? C - 1 - i : i;
+                O[it] *= ro.sc_o;
+                if (tail && t0 + j >= len) O[it] = v4f{0.f, 0.f, 0.f, 0.f};
+                if constexpr (DOTS) {
+                    float dot = 0.f;
 #pragma unroll
-                for (int ct = 0; ct < CT; ++ct) {
-                    const int nn = n0 + ct * 16 + 4 * g;
-                    v4f o = O[it][ct] * ro.sc_o;
-                    if (!live) o = v4f{0.f, 0.f, 0.f, 0.f};
-                    if (t < a.T && nn < ro.N) {
-                        const size_t at = (((size_t)b * a.T + t) * a.H + h) * ro.N + nn;
-                        if (ro.out_f32) {
-                            float *p = (float *)ro.out + at;
-                            if (ro.N % 4 == 0) *(v4f *)p = o;
-                            else
-                                for (int r = 0; r < 4; ++r)
-                                    if (nn + r < ro.N) p[r] = o[r];
-                        } else {
-                            T *p = (T *)ro.out + at;
-                            typedef T v4t __attribute__((ext_vector_type(4)));
-                            const v4t y = {Ty::down(o[0]), Ty::down(o[1]), Ty::down(o[2]), Ty::down(o[3])};
-                            if (ro.wide_out) *(v4t *)p = y;
-                            else
-                                for (int r = 0; r < 4; ++r)
-                                    if (nn + r < ro.N) p[r] = y[r];
-                        }
-                    }
-                    if (ro.dot && live) {
-                        const T *p = (const T *)ro.partner.p + b * ro.partner.sb + t * ro.partner.st +
-                                     (h / ro.partner.r) * ro.partner.sh + nn;
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (nn + r < ro.N) dot = fmaf(o[r], Ty::up(p[r]), dot);
-                    }
-                }
-                if (ro.dot) {
+                    for (int r = 0; r < 4; ++r) dot = fmaf(O[it][r], Ty::up(pr[it][r]), dot);
                     dot = group_sum(dot);
                     if (g == 0) dots[w * C + i] = dot;
                 }
             }
+            const int rows = a.T - t0 < C ? a.T - t0 : C;
+            const size_t first = (((size_t)b * a.T + t0) * a.H + h) * N;
+            const auto ors = bounded_rsrc((char *)ro.out + first * out_size,
+                                          (uint32_t)((rows - 1) * out_row + N * out_size));
+            const int l = afresh(lane);
+#pragma unroll
+            for (int it = 0; it < NT; ++it) {
+                const v4f o = O[it];
+                const int off = (int)out_off(l, it, out_row, out_size);
+                const bool four = sizeof(T) == 4 || ro.out_f32;
+                union { T x[4]; uint16_t h[4]; v2u u; } y;
+                if constexpr (sizeof(T) == 2)
+                    for (int r = 0; r < 4; ++r) y.x[r] = Ty::down(o[r]);
+                if (ro.wide_out) {
+                    if (four) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, o), ors, off, 0, 0);
+                    else __builtin_amdgcn_raw_buffer_store_b64(y.u, ors, off, 0, 0);
+                    continue;
+                }
+                const int nn = n0 + 4 * (l >> 4);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int at = nn + r < N ? off + r * out_size : (int)kOutside;
+                    if (four) bstore_u(ors, __float_as_uint(o[r]), (uint32_t)at, 0);
+                    else __builtin_amdgcn_raw_buffer_store_b16(y.h[r], ors, at, 0, 0);
+                }
+            }
         }
-        if (OUT && anc && !rev) put_state(anc, ro.N, 1, 1.f);
+        if constexpr (DOTS)
+            if (anc && !rev) put_state(anc, N, 1, 1.f);
         lds_barrier();
-        if (OUT && ro.dot && (int)threadIdx.x < C) {
-            const int i = threadIdx.x, t = rev ? t0 + C - 1 - i : t0 + i;
-            if (t < a.T)
-                ro.dot[((size_t)tile * a.B * a.H + bh) * a.T + t] =
-                    (dots[i] + dots[C + i]) + (dots[2 * C + i] + dots[3 * C + i]);
+        if constexpr (DOTS) {
+            if ((int)threadIdx.x < C) {
+                const int i = threadIdx.x, t = rev ? t0 + C - 1 - i : t0 + i;
+                if (t < a.T) {
+                    float d = 0.f;
+#pragma unroll
+                    for (int k = 0; k < NW; ++k) d += dots[k * C + i];
+                    ro.dot[((size_t)tile * a.B * a.H + bh) * a.T + t] = d;
+                }
+            }
+            lds_barrier();   // (q's next rows go where the dots were)
         }
     }
 
@@ -533,16 +635,16 @@ __global__ __launch_bounds__(256, (LinTile<InParts<Ty>::n, KT, CW, NPX, OUT>::wa
             put_state(ro.fin + bh * mat, ro.fin_d, ro.fin_n, f);
         }
     } else {
-        put_state(ro.seg + ((size_t)bh * a.nseg + seg) * mat, ro.N, 1, 1.f);
-        if (w == 3 && lane == 0 && tile == 0) ro.seg_decay[(size_t)bh * a.nseg + seg] = __builtin_amdgcn_exp2f((float)total);
+        put_state(ro.seg + ((size_t)bh * a.nseg + seg) * mat, N, 1, 1.f);
+        if (w == NW - 1 && lane == 0 && tile == 0) ro.seg_decay[(size_t)bh * a.nseg + seg] = __builtin_amdgcn_exp2f((float)total);
     }
 }
 
 // ---- launches -------------------------------------------------------------------------------------
 
-template <class Ty, int KT, int CW, int NPX, bool OUT>
+template <class Ty, int KT, int NW, int NPX, int MODE>
 int launch_walk_tile(const LinArgs &a, const LinRole *roles, int n, hipStream_t st) {
-    using Tile = LinTile<InParts<Ty>::n, KT, CW, NPX, OUT>;
+    using Tile = LinTile<InParts<Ty>::n, KT, NW, NPX, MODE>;
     LinRoles rs{};
     int tiles = 0;
     for (int i = 0; i < n; ++i) {
@@ -550,29 +652,27 @@ int launch_walk_tile(const LinArgs &a, const LinRole *roles, int n, hipStream_t 
         const int t = (roles[i].N + Tile::NB - 1) / Tile::NB;
         tiles = t > tiles ? t : tiles;
     }
-    const void *fn = (const void *)k_lin_walk<Ty, KT, CW, NPX, OUT>;
+    const void *fn = (const void *)k_lin_walk<Ty, KT, NW, NPX, MODE>;
     if (Tile::lds > 64 * 1024) DEER_HIP(hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, Tile::lds));
-    KTimer kt(OUT ? "k_lin_walk" : "k_lin_walk_states", st);
-    hipLaunchKernelGGL((k_lin_walk<Ty, KT, CW, NPX, OUT>), dim3((unsigned)(a.B * a.H * a.nseg * tiles), n), dim3(256),
+    KTimer kt(MODE == kStates ? "k_lin_walk_states" : "k_lin_walk", st);
+    hipLaunchKernelGGL((k_lin_walk<Ty, KT, NW, NPX, MODE>), dim3((unsigned)(a.B * a.H * a.nseg * tiles), n), dim3(64 * NW),
                        Tile::lds, st, a, rs);
     DEER_LAUNCH_CHECK("k_lin_walk");
     return DEER_OK;
 }
 
-template <class Ty, int NPX, bool OUT>
+template <class Ty, int NPX, int MODE>
 int launch_walk_parts(const LinArgs &a, const LinRole *roles, int n, hipStream_t st) {
-    constexpr int NPI = InParts<Ty>::n;
-    const int KT = kt_of(roles[0].Kd), CW = cw_of(NPI, KT, roles[0].N);
-    if (KT == 256) return launch_walk_tile<Ty, 256, 16, NPX, OUT>(a, roles, n, st);
-    if (CW == 16) {
-        if (KT == 32) return launch_walk_tile<Ty, 32, 16, NPX, OUT>(a, roles, n, st);
-        if (KT == 64) return launch_walk_tile<Ty, 64, 16, NPX, OUT>(a, roles, n, st);
-        return launch_walk_tile<Ty, 128, 16, NPX, OUT>(a, roles, n, st);
+    const int KT = kt_of(roles[0].Kd), NW = nw_of(KT, roles[0].N);
+    if (KT == 256) return launch_walk_tile<Ty, 256, 4, NPX, MODE>(a, roles, n, st);
+    if (NW == 4) {
+        if (KT == 32) return launch_walk_tile<Ty, 32, 4, NPX, MODE>(a, roles, n, st);
+        if (KT == 64) return launch_walk_tile<Ty, 64, 4, NPX, MODE>(a, roles, n, st);
+        return launch_walk_tile<Ty, 128, 4, NPX, MODE>(a, roles, n, st);
     }
-    if (KT == 32) return launch_walk_tile<Ty, 32, 32, NPX, OUT>(a, roles, n, st);
-    if (KT == 64) return launch_walk_tile<Ty, 64, 32, NPX, OUT>(a, roles, n, st);
-    if constexpr (NPI < 3) return launch_walk_tile<Ty, 128, 32, NPX, OUT>(a, roles, n, st);
-    return DEER_ERR_INVALID_ARG;
+    if (KT == 32) return launch_walk_tile<Ty, 32, 8, NPX, MODE>(a, roles, n, st);
+    if (KT == 64) return launch_walk_tile<Ty, 64, 8, NPX, MODE>(a, roles, n, st);
+    return launch_walk_tile<Ty, 128, 8, NPX, MODE>(a, roles, n, st);
 }
 
 }  // namespace deer
