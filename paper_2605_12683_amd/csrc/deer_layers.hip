@@ -1,6 +1,7 @@
 // C ABI of the layers: linear attention with decays and layer normalisation (argument checks,
 // workspace, the operands of each walk).  All device work is queued on the caller's stream.
 #include <math.h>
+#include <stdlib.h>
 
 #include "common.h"
 #include "launch.h"
@@ -47,16 +48,24 @@ static LinView view_of(const deer_view *x, int r, int T) {
     return {x->p, (long)x->sb, T > 1 ? (long)x->st : 0, (long)x->sh, r};
 }
 
-// Segments: enough that the walks' blocks fill the chip twice (two blocks share a CU), none of
-// fewer than kMinSeg steps; one where the walks alone give half of that, since further segments
-// read k and v a second time.
-constexpr int kFillBlocks = 512, kMinSeg = 256;
+// DEER_LIN_SEG=n: segments of n steps (rounded up to 64), whatever the sizes (a tuning and test
+// override)
+static int seg_override() {
+    const char *e = getenv("DEER_LIN_SEG");
+    return e ? atoi(e) : 0;
+}
+
+// Segments: enough that the walks fill the chip with kFillWaves waves (four a SIMD), none of fewer
+// than kMinSeg steps; one where the walks alone give half of that, since further segments read k and
+// v a second time.
+constexpr int kFillWaves = 4096, kMinSeg = 256;
 
 static int segment_steps(const deer_linattn_shape *s, int B, int T, int op) {
-    long blocks = (long)B * s->H * lin_tiles(s->Dk, s->Dv);
-    if (op == DEER_OP_ADJOINT) blocks += 2L * B * s->H * lin_tiles(s->Dv, s->Dk);
-    if (2 * blocks >= kFillBlocks || T <= kMinSeg) return T;
-    const long n = (kFillBlocks + blocks - 1) / blocks;
+    if (const int n = seg_override(); n > 0) return n >= T ? T : (n + 63) / 64 * 64;
+    long waves = (long)B * s->H * lin_waves(s->Dk, s->Dv);
+    if (op == DEER_OP_ADJOINT) waves += 2L * B * s->H * lin_waves(s->Dv, s->Dk);
+    if (2 * waves >= kFillWaves || T <= kMinSeg) return T;
+    const long n = (kFillWaves + waves - 1) / waves;
     const long steps = ((T + n - 1) / n + 63) / 64 * 64;
     return (int)(steps < kMinSeg ? kMinSeg : steps);
 }

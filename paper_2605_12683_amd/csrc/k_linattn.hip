@@ -69,6 +69,8 @@ int lin_tiles(int Kd, int N) {
     return (N + nb - 1) / nb;
 }
 
+int lin_waves(int Kd, int N) { return lin_tiles(Kd, N) * nw_of(kt_of(Kd), N); }
+
 bool lin_same_tile(int Kd, int N, int Kd2, int N2) {
     return kt_of(Kd) == kt_of(Kd2) && nw_of(kt_of(Kd), N) == nw_of(kt_of(Kd2), N2);
 }

@@ -364,6 +364,7 @@ struct LinArgs {
     int seg_steps, nseg;        // segments of seg_steps steps (a multiple of 64), or one of all T
 };
 int lin_tiles(int Kd, int N);   // blocks that share the N columns of one head's state
+int lin_waves(int Kd, int N);              // their waves
 bool lin_same_tile(int Kd, int N, int Kd2, int N2);
 // all roles of one call have the same tile shape; states: what each segment adds (into seg,
 // seg_decay), else the outputs; dots: and dot, anchor (which are summed over many steps, so the

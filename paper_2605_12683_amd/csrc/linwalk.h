@@ -86,9 +86,10 @@ struct LinTile {
     static constexpr bool OUT = MODE != kStates;
     static constexpr int NB = 16 * NW, TH = 64 * NW;
     static constexpr int PQ = KT + 8, PK = KT + 16, PV = NB + 16;   // LDS row pitches: no bank conflicts
-    static constexpr int bytes(int C) {   // (the dots lie where q was)
-        return NPI * C * 2 * ((OUT ? PQ : 0) + PK + PV) + (OUT ? (C / 16) * (C / 32) * NPX * 1024 : 0) +
-               2 * (4 * C + 4) * 4;
+    static constexpr int pairs(int C) { return C == 64 ? 6 : 2; }   // (16 outputs, 32 sources) not all above the diagonal
+    static constexpr int bytes(int C) {
+        return NPI * C * 2 * ((OUT ? PQ : 0) + PK + PV) + (OUT ? pairs(C) * NPX * 1024 : 0) + 2 * (4 * C + 4) * 4 +
+               (MODE == kOutDots ? NW * C * 4 : 0);
     }
     static constexpr int C = bytes(64) <= 80 * 1024 ? 64 : 32;
     static constexpr int lds = bytes(C);
@@ -124,33 +125,29 @@ struct RowTile {
     using T = typename Ty::T;
     static constexpr int E = 16 / sizeof(T), UPR = W / E, NU = (C * UPR + TH - 1) / TH, ROWS = TH / UPR;
     const T *base;
-    int st, width, step, d;        // st, step in bytes
-    uint32_t off;
+    int st, col0, width;           // st in bytes
     bool fast, rev;
     v4u u[NU];
 
-    __device__ __forceinline__ void init(const LinView &x, int b, int h, int col0, int width_, bool rev_) {
+    __device__ __forceinline__ void init(const LinView &x, int b, int h, int col0_, int width_, bool rev_) {
         base = (const T *)x.p + b * x.sb + (h / x.r) * x.sh;
-        st = (int)(x.st * (long)sizeof(T)), width = width_, rev = rev_;
+        st = (int)(x.st * (long)sizeof(T)), col0 = col0_, width = width_, rev = rev_;
         fast = (((uintptr_t)base | (uintptr_t)st) & 15) == 0 && width % E == 0 && x.st >= width;
-        const int row = threadIdx.x / UPR;
-        d = col0 + (threadIdx.x % UPR) * E;
-        step = rev ? -ROWS * st : ROWS * st;
-        off = d < width && row < C ? (uint32_t)((rev ? C - 1 - row : row) * st + d * (int)sizeof(T)) : kOutside;
     }
 
     __device__ __forceinline__ void load(int t0, int len) {
         const int rows = len - t0 < C ? len - t0 : C;
         const auto rs = bounded_rsrc((const char *)base + (long)t0 * st,
                                      rows > 0 ? (uint32_t)((rows - 1) * st + width * (int)sizeof(T)) : 0u);
-        const uint32_t o = (uint32_t)afresh((int)off);
+        const int tid = afresh((int)threadIdx.x), r0 = tid / UPR, d = col0 + (tid % UPR) * E;
+        const int step = rev ? -ROWS * st : ROWS * st;
+        const uint32_t o = d < width && r0 < C ? (uint32_t)((rev ? C - 1 - r0 : r0) * st + d * (int)sizeof(T)) : kOutside;
         if (fast) {
 #pragma unroll
             for (int i = 0; i < NU; ++i)
                 u[i] = __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)(o + (uint32_t)(i * step)), 0, 0));
             return;
         }
-        const int r0 = afresh((int)(threadIdx.x / UPR));
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
             const int row = i * ROWS + r0, j = rev ? C - 1 - row : row;
@@ -172,9 +169,10 @@ struct RowTile {
     template <bool PERM>
     __device__ __forceinline__ void store(uint16_t *lds, int pitch) const {
         constexpr int NP = InParts<Ty>::n;
+        const int tid = afresh((int)threadIdx.x);
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
-            const int n = i * TH + threadIdx.x, row = n / UPR, d = (n % UPR) * E;
+            const int n = i * TH + tid, row = n / UPR, d = (n % UPR) * E;
             if (C * UPR % TH != 0 && row >= C) continue;
 #pragma unroll
             for (int half = 0; half < E / 4; ++half) {   // four elements at a time
@@ -306,20 +304,26 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, NPX, MODE
     constexpr bool OUT = Tile::OUT, DOTS = MODE == kOutDots;
     constexpr int C = Tile::C, NB = Tile::NB, TH = Tile::TH, PQ = Tile::PQ, PK = Tile::PK, PV = Tile::PV;
     constexpr int NT = C / 16, KS = C / 32, DT = KT / 16;
+    // operands read from LDS at a time: as many as the registers hold twice (dividing NT, DT)
+    constexpr bool TIGHT = KT == 128 && NW == 8;
+    constexpr int UB = TIGHT && DOTS ? 1 : KT / 32 * NPI <= 4 ? KT / 32 : NPI == 1 ? 4 : NPI == 2 ? 2 : 1;
+    constexpr int QB = TIGHT ? 2 : NT, KB = NPI == 1 && !TIGHT && DT > 2 ? 4 : 2, PB = NPX == 2 && !TIGHT ? 2 : 1;
     extern __shared__ __align__(16) unsigned char smem[];
     uint16_t *Ks = (uint16_t *)smem, *Vs = Ks + NPI * C * PK, *Qs = Vs + NPI * C * PV;
     unsigned char *rest = (unsigned char *)(Qs + (OUT ? NPI * C * PQ : 0));
-    v4u *Ps = (v4u *)rest;                                     // [NT][KS][NPX][64 lanes]
-    Decays<C> *dec = (Decays<C> *)(rest + (OUT ? NT * KS * NPX * 1024 : 0));
-    float *dots = (float *)Qs;                                 // [NW][C], between the chunk's last two barriers
+    constexpr int PAIRS = Tile::pairs(C);
+    v4u *Ps = (v4u *)rest;                                     // [PAIRS][NPX][64 lanes]
+    auto pair = [](int it, int ks) { return it < 2 ? it : 2 * it - 2 + ks; };
+    Decays<C> *dec = (Decays<C> *)(rest + (OUT ? PAIRS * NPX * 1024 : 0));
+    float *dots = (float *)(dec + 2);                          // [NW][C]
 
-    const LinRole &ro = rs.r[blockIdx.y];
+    const LinRole ro = rs.r[blockIdx.y];
     const int tiles = (ro.N + NB - 1) / NB;
     const long units = (long)a.B * a.H * a.nseg * tiles;
     if ((long)blockIdx.x >= units) return;
     const int tile = blockIdx.x % tiles, seg = blockIdx.x / tiles % a.nseg, bh = blockIdx.x / tiles / a.nseg;
     const int b = bh / a.H, h = bh % a.H;
-    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const bool rev = ro.reverse;
     const int len = length_of(a, b);
     const int lo = seg * a.seg_steps, hi = lo + a.seg_steps < a.T ? lo + a.seg_steps : a.T;
@@ -345,7 +349,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, NPX, MODE
     };
     auto gate = [&](int n) {
         if (n >= chunks) return 0.f;
-        const int i = lane & (C - 1);
+        const int i = threadIdx.x & (C - 1);
         return gate_raw(a, b, h, t0_of(n) + (rev ? C - 1 - i : i), len, rev);
     };
 
@@ -370,7 +374,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, NPX, MODE
     }
     auto put_state = [&](float *dst, int sd, int sn, float f) {
         const auto rsrc = bounded_rsrc(dst, (uint32_t)(mat * 4));
-        const int l = afresh(lane);
+        const int l = afresh((int)threadIdx.x) & 63;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -397,28 +401,37 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, NPX, MODE
 
     // tiles above the diagonal that share an operand with one on it stay zero
     if constexpr (OUT)
-        for (int i = threadIdx.x; i < NT * KS * NPX * 64; i += TH) Ps[i] = v4u{0, 0, 0, 0};
+        for (int i = threadIdx.x; i < PAIRS * NPX * 64; i += TH) Ps[i] = v4u{0, 0, 0, 0};
+    auto store = [&] {
+        kr.template store<false>(Ks, PK);
+        vr.template store<false>(Vs, PV);
+        if constexpr (OUT) qr.template store<true>(Qs, PQ);
+    };
     load(0);
     double total = 0.0;                                        // last wave: log2 decay of the segment
     float raw = 0.f;
     if (w == NW - 1) {
-        total += chunk_decays<C>(dec[0], gate(0), ro.sc_kv);
-        raw = gate(1);
+        const double L = chunk_decays<C>(dec[0], gate(0), ro.sc_kv);
+        if (!OUT) total += L;
+        raw = __int_as_float(afresh(__float_as_int(gate(1))));
     }
     const int na = (a.T + kLinAnchor - 1) / kLinAnchor;
 
+    store();
+
+    // The next chunk's rows are loaded while this one is computed and go to LDS before this one's
+    // results go out: the wait for loads is then never one for stores too.
     for (int n = 0; n < chunks; ++n) {
         const int t0 = t0_of(n);
         const Decays<C> &dc = dec[n & 1];
-        kr.template store<false>(Ks, PK);
-        vr.template store<false>(Vs, PV);
-        if constexpr (OUT) qr.template store<true>(Qs, PQ);
         lds_barrier();
         if (n + 1 < chunks) {
+            const float next = raw;
+            if (w == NW - 1) raw = gate(n + 2);
             load(n + 1);
             if (w == NW - 1) {
-                total += chunk_decays<C>(dec[(n + 1) & 1], raw, ro.sc_kv);
-                raw = gate(n + 2);
+                const double L = chunk_decays<C>(dec[(n + 1) & 1], next, ro.sc_kv);
+                if (!OUT) total += L;
             }
         }
         float *anc = nullptr;
@@ -432,30 +445,36 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, NPX, MODE
         if constexpr (OUT) {
             // decayed scores, transposed: rows j, columns i
             for (int tl = w; tl < NT * (NT + 1) / 2; tl += NW) {
+                const int lane = afresh((int)threadIdx.x) & 63, g = lane >> 4, c = lane & 15;
                 const int it = tl >= 6 ? 3 : tl >= 3 ? 2 : tl >= 1 ? 1 : 0, jt = tl - it * (it + 1) / 2;
-                v4f acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int u = 0; u < KT / 32; ++u) {
-                    v4u kf[NPI], qf[NPI];
-#pragma unroll
-                    for (int p = 0; p < NPI; ++p) {
-                        const uint16_t *kp = Ks + (p * C + jt * 16 + c) * PK + u * 32 + 4 * g;
-                        const v2u k0 = *(const v2u *)kp, k1 = *(const v2u *)(kp + 16);
-                        kf[p] = v4u{k0[0], k0[1], k1[0], k1[1]};
-                        qf[p] = *(const v4u *)(Qs + (p * C + it * 16 + c) * PQ + u * 32 + 8 * g);
-                    }
-                    acc = mfma_parts<NPI - 1>(kf, qf, acc);
-                }
                 const int i = it * 16 + c, j0 = jt * 16 + 4 * g;
                 const float hi_i = dc.hi[i], lo_i = dc.lo[i];
+                const v4f hi_j = *(const v4f *)(dc.hi + j0), lo_j = *(const v4f *)(dc.lo + j0);
+                v4f acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int u0 = 0; u0 < KT / 32; u0 += UB) {   // reads of UB products at a time
+                    v4u kf[UB][NPI], qf[UB][NPI];
+#pragma unroll
+                    for (int u = 0; u < UB; ++u)
+#pragma unroll
+                        for (int p = 0; p < NPI; ++p) {
+                            const uint16_t *kp = Ks + (p * C + jt * 16 + c) * PK + (u0 + u) * 32 + 4 * g;
+                            const v2u k0 = *(const v2u *)kp, k1 = *(const v2u *)(kp + 16);
+                            kf[u][p] = v4u{k0[0], k0[1], k1[0], k1[1]};
+                            qf[u][p] = *(const v4u *)(Qs + (p * C + it * 16 + c) * PQ + (u0 + u) * 32 + 8 * g);
+                        }
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int u = 0; u < UB; ++u) acc = mfma_parts<NPI - 1>(kf[u], qf[u], acc);
+                }
                 float x[4];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const float e = (hi_i - dc.hi[j0 + r]) + (lo_i - dc.lo[j0 + r]);
+                    const float e = (hi_i - hi_j[r]) + (lo_i - lo_j[r]);
                     const float p = acc[r] * ro.sc_kv * __builtin_amdgcn_exp2f(e);
                     x[r] = j0 + r <= i ? p : 0.f;
                 }
-                uint32_t *dst = (uint32_t *)(Ps + ((it * KS + (jt >> 1)) * NPX) * 64 + lane) + (jt & 1) * 2;
+                uint32_t *dst = (uint32_t *)(Ps + pair(it, jt >> 1) * NPX * 64 + lane) + (jt & 1) * 2;
                 uint32_t p0[3], p1[3];
                 split_pair(x[0], x[1], p0);
                 split_pair(x[2], x[3], p1);
@@ -463,37 +482,48 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, NPX, MODE
                 for (int q = 0; q < NPX; ++q) *(v2u *)(dst + q * 64 * 4) = v2u{p0[q], p1[q]};
             }
             // what the entering state gives, transposed: rows n, columns i
+            const int lane = afresh((int)threadIdx.x) & 63, g = lane >> 4, c = lane & 15;
 #pragma unroll
             for (int it = 0; it < NT; ++it) O[it] = v4f{0.f, 0.f, 0.f, 0.f};
+            v4u qf[2][QB][NPI];   // read QB at a time, one time ahead
+            auto read_q = [&](int n) {
+                const int u = n / (NT / QB), it0 = n % (NT / QB) * QB;
 #pragma unroll
-            for (int u = 0; u < KT / 32; ++u) {
-                v4u sf[NPX];
-                float x[8];
+                for (int m = 0; m < QB; ++m)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) x[r] = S[2 * u][r], x[4 + r] = S[2 * u + 1][r];
-                split8<NPX>(x, sf);
+                    for (int p = 0; p < NPI; ++p)
+                        qf[n & 1][m][p] = *(const v4u *)(Qs + (p * C + (it0 + m) * 16 + c) * PQ + u * 32 + 8 * g);
+            };
+            constexpr int QN = KT / 32 * (NT / QB);
+            read_q(0);
+            v4u sf[NPX];
 #pragma unroll
-                for (int it = 0; it < NT; ++it) {
-                    v4u qf[NPI];
+            for (int n = 0; n < QN; ++n) {
+                const int u = n / (NT / QB), it0 = n % (NT / QB) * QB;
+                if (n + 1 < QN) read_q(n + 1);
+                __builtin_amdgcn_sched_barrier(0);
+                if (it0 == 0) {
+                    float x[8];
 #pragma unroll
-                    for (int p = 0; p < NPI; ++p) qf[p] = *(const v4u *)(Qs + (p * C + it * 16 + c) * PQ + u * 32 + 8 * g);
-                    O[it] = mfma_parts<NPX - 1>(sf, qf, O[it]);
+                    for (int r = 0; r < 4; ++r) x[r] = S[2 * u][r], x[4 + r] = S[2 * u + 1][r];
+                    split8<NPX>(x, sf);
                 }
-                __builtin_amdgcn_sched_barrier(0);   // (parts of one 32 rows of the state at a time)
+#pragma unroll
+                for (int m = 0; m < QB; ++m) O[it0 + m] = mfma_parts<NPX - 1>(sf, qf[n & 1][m], O[it0 + m]);
+                __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
             for (int it = 0; it < NT; ++it) O[it] *= dc.from[it * 16 + c];
             lds_barrier();
         }
 
-        // the partner's rows, used at the end
         typedef T v4t __attribute__((ext_vector_type(4)));
-        v4t pr[DOTS ? NT : 1];
-        if constexpr (DOTS) {
+        v4t pr[DOTS ? NT : 1];        // the partner's rows, used at the end
+        auto read_partner = [&] {
             const int rows = len - t0 < C ? len - t0 : C;
             const auto prs = bounded_rsrc(partner + t0 * ro.partner.st,
                                           rows > 0 ? (uint32_t)(((rows - 1) * ro.partner.st + N) * sizeof(T)) : 0u);
-            const int row = (int)(ro.partner.st * (long)sizeof(T)), l = afresh(lane);
+            const int row = (int)(ro.partner.st * (long)sizeof(T)), l = afresh((int)threadIdx.x) & 63;
 #pragma unroll
             for (int it = 0; it < NT; ++it) {
                 const int off = (int)out_off(l, it, row, sizeof(T));
@@ -512,9 +542,10 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, NPX, MODE
                         pr[it][r] = bload(prs, (uint32_t)at, 0);
                     else
                         pr[it][r] = __builtin_bit_cast(T, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(prs, at, 0, 0));
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
-        }
+        };
 
         // the chunk's own steps, and the state at its end
         const float all = dc.all;
@@ -522,6 +553,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, NPX, MODE
         for (int dt = 0; dt < DT; ++dt) S[dt] *= all;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
+            const int lane = afresh((int)threadIdx.x) & 63, g = lane >> 4, c = lane & 15;
             v4u vf[NPI], sv[3];
             float x[8];
 #pragma unroll
@@ -544,33 +576,64 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, NPX, MODE
                 x[4 + r] *= dc.into[ks * 32 + 16 + 4 * g + r];
             }
             split8<3>(x, sv);
-            __builtin_amdgcn_sched_barrier(0);
+
+            // products of the scores with v, then of k with the decayed v, KB of each at a time, the
+            // operands of the next ones read while these run
+            constexpr int PN = (NT + PB - 1) / PB;
+            v4u pf[2][PB][NPX], kf[2][KB][NPI];
+            auto read_p = [&](int n) {
+#pragma unroll
+                for (int m = 0; m < PB; ++m) {
+                    const int it = 2 * ks + n * PB + m;
+                    if (it < NT)
+#pragma unroll
+                        for (int q = 0; q < NPX; ++q) pf[n & 1][m][q] = Ps[(pair(it, ks) * NPX + q) * 64 + lane];
+                }
+            };
+            auto read_k = [&](int n) {
+#pragma unroll
+                for (int m = 0; m < KB; ++m)
+#pragma unroll
+                    for (int p = 0; p < NPI; ++p) {
+                        const uint16_t *kp = Ks + p * C * PK;
+                        const v2u k0 = read_turned(kp, PK, ks * 32, (n * KB + m) * 16, g, c);
+                        const v2u k1 = read_turned(kp, PK, ks * 32 + 16, (n * KB + m) * 16, g, c);
+                        kf[n & 1][m][p] = v4u{k0[0], k0[1], k1[0], k1[1]};
+                    }
+            };
             if constexpr (OUT) {
+                read_p(0);
 #pragma unroll
-                for (int it = 2 * ks; it < NT; ++it) {
-                    v4u pf[NPX];
+                for (int n = 0; n < PN; ++n) {
+                    if (2 * ks + n * PB >= NT) break;
+                    if (2 * ks + (n + 1) * PB < NT) read_p(n + 1);
+                    else read_k(0);
+                    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int q = 0; q < NPX; ++q) pf[q] = Ps[((it * KS + ks) * NPX + q) * 64 + lane];
-                    O[it] = mfma_parts<NPX - 1>(vf, pf, O[it]);
+                    for (int m = 0; m < PB; ++m) {
+                        const int it = 2 * ks + n * PB + m;
+                        if (it < NT) O[it] = mfma_parts<NPX - 1>(vf, pf[n & 1][m], O[it]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
+            } else {
+                read_k(0);
             }
+            if constexpr (DOTS)
+                if (ks == KS - 1) read_partner();
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) {
-                v4u kf[NPI];
+            for (int n = 0; n < DT / KB; ++n) {
+                if (n + 1 < DT / KB) read_k(n + 1);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int p = 0; p < NPI; ++p) {
-                    const uint16_t *kp = Ks + p * C * PK;
-                    const v2u k0 = read_turned(kp, PK, ks * 32, dt * 16, g, c);
-                    const v2u k1 = read_turned(kp, PK, ks * 32 + 16, dt * 16, g, c);
-                    kf[p] = v4u{k0[0], k0[1], k1[0], k1[1]};
-                }
-                S[dt] = mfma_parts<2>(kf, sv, S[dt]);
-                if (dt % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+                for (int m = 0; m < KB; ++m) S[n * KB + m] = mfma_parts<2>(kf[n & 1][m], sv, S[n * KB + m]);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
 
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (OUT) {
+            const int lane = afresh((int)threadIdx.x) & 63, g = lane >> 4, c = lane & 15;
             const bool tail = t0 + C > len;      // some rows lie behind the sequence's end: zero
 #pragma unroll
             for (int it = 0; it < NT; ++it) {
@@ -585,11 +648,20 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, NPX, MODE
                     if (g == 0) dots[w * C + i] = dot;
                 }
             }
+        }
+        if constexpr (DOTS)
+            if (anc && !rev) put_state(anc, N, 1, 1.f);
+        lds_barrier();
+        if (n + 1 < chunks) {
+            store();
+            raw = __int_as_float(afresh(__float_as_int(raw)));   // (loaded before the rows: no wait for it later)
+        }
+        if constexpr (OUT) {
             const int rows = a.T - t0 < C ? a.T - t0 : C;
             const size_t first = (((size_t)b * a.T + t0) * a.H + h) * N;
             const auto ors = bounded_rsrc((char *)ro.out + first * out_size,
                                           (uint32_t)((rows - 1) * out_row + N * out_size));
-            const int l = afresh(lane);
+            const int l = afresh((int)threadIdx.x) & 63;
 #pragma unroll
             for (int it = 0; it < NT; ++it) {
                 const v4f o = O[it];
@@ -612,20 +684,14 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, NPX, MODE
                 }
             }
         }
-        if constexpr (DOTS)
-            if (anc && !rev) put_state(anc, N, 1, 1.f);
-        lds_barrier();
         if constexpr (DOTS) {
-            if ((int)threadIdx.x < C) {
-                const int i = threadIdx.x, t = rev ? t0 + C - 1 - i : t0 + i;
-                if (t < a.T) {
-                    float d = 0.f;
+            const int i = threadIdx.x, t = rev ? t0 + C - 1 - i : t0 + i;
+            if (i < C && t < a.T) {
+                float d = 0.f;
 #pragma unroll
-                    for (int k = 0; k < NW; ++k) d += dots[k * C + i];
-                    ro.dot[((size_t)tile * a.B * a.H + bh) * a.T + t] = d;
-                }
+                for (int k = 0; k < NW; ++k) d += dots[k * C + i];
+                ro.dot[((size_t)tile * a.B * a.H + bh) * a.T + t] = d;
             }
-            lds_barrier();   // (q's next rows go where the dots were)
         }
     }
 
