@@ -55,17 +55,19 @@ static int seg_override() {
     return e ? atoi(e) : 0;
 }
 
-// Segments: enough that the walks fill the chip with kFillWaves waves (four a SIMD), none of fewer
-// than kMinSeg steps; one where the walks alone give half of that, since further segments read k and
-// v a second time.
-constexpr int kFillWaves = 4096, kMinSeg = 256;
+// Segments: enough that a walk's blocks fill the chip twice (two share a CU), none of fewer than
+// kMinSeg steps; one where the heads alone give half of that, since segments read k and v a second
+// time.  (2 x 4096 steps, 16 heads of 128 x 128 in bf16, where one segment gives 32 blocks: segments
+// of 256, 512, 1024, 4096 steps take 81, 79, 125, 304 us.)
+constexpr int kFillBlocks = 512, kMinSeg = 256;
 
 static int segment_steps(const deer_linattn_shape *s, int B, int T, int op) {
     if (const int n = seg_override(); n > 0) return n >= T ? T : (n + 63) / 64 * 64;
-    long waves = (long)B * s->H * lin_waves(s->Dk, s->Dv);
-    if (op == DEER_OP_ADJOINT) waves += 2L * B * s->H * lin_waves(s->Dv, s->Dk);
-    if (2 * waves >= kFillWaves || T <= kMinSeg) return T;
-    const long n = (kFillWaves + waves - 1) / waves;
+    // the adjoint's walks of dq and dk run together, that of dv by itself
+    long blocks = (long)B * s->H * lin_tiles(s->Dk, s->Dv);
+    if (op == DEER_OP_ADJOINT) blocks = 2L * B * s->H * lin_tiles(s->Dv, s->Dk);
+    if (2 * blocks >= kFillBlocks || T <= kMinSeg) return T;
+    const long n = (kFillBlocks + blocks - 1) / blocks;
     const long steps = ((T + n - 1) / n + 63) / 64 * 64;
     return (int)(steps < kMinSeg ? kMinSeg : steps);
 }
@@ -117,9 +119,8 @@ static LinWs carve_lin(void *ws, const deer_linattn_shape *s, int B, int T, int 
     return w;
 }
 
-static bool wide_out(const void *p, int dtype, int N) {
-    return N % 4 == 0 && ((uintptr_t)p & (4 * dtype_size(dtype) - 1)) == 0;
-}
+// whether out's rows of N take 16-byte stores of eight elements (or two of four)
+static bool wide_out(const void *p, int N) { return N % 8 == 0 && ((uintptr_t)p & 15) == 0; }
 
 static int check_norm(const deer_norm *n, int64_t rows) {
     if (!n) { set_error("norm pointer is NULL"); return DEER_ERR_INVALID_ARG; }
@@ -172,7 +173,7 @@ int deer_linattn(const deer_linattn_shape *s, int B, int T, const deer_view *q, 
     ro.q = view_of(q, r, T), ro.k = view_of(k, r, T), ro.v = view_of(v, 1, T);
     ro.Kd = s->Dk, ro.N = s->Dv;
     ro.sc_kv = 1.f, ro.sc_o = s->scale;
-    ro.out = o, ro.wide_out = wide_out(o, s->dtype, s->Dv);
+    ro.out = o, ro.wide_out = wide_out(o, s->Dv);
     ro.init = state0, ro.init_d = s->Dv, ro.init_n = 1;
     ro.fin = state, ro.fin_d = s->Dv, ro.fin_n = 1;
     if (a.nseg > 1) {
@@ -211,7 +212,7 @@ int deer_linattn_adjoint(const deer_linattn_shape *s, int B, int T, const deer_v
     ro[0].q = vg, ro[0].k = vv, ro[0].v = vk;
     ro[0].Kd = Dv, ro[0].N = Dk;
     ro[0].sc_kv = 1.f, ro[0].sc_o = s->scale;
-    ro[0].out = shared ? (void *)w.dq : dq, ro[0].out_f32 = shared, ro[0].wide_out = wide_out(dq, s->dtype, Dk);
+    ro[0].out = shared ? (void *)w.dq : dq, ro[0].out_f32 = shared, ro[0].wide_out = wide_out(ro[0].out, Dk);
     ro[0].init = state0, ro[0].init_d = 1, ro[0].init_n = Dv;
     if (decay) ro[0].partner = vq, ro[0].dot = w.dq_dot, ro[0].anchor = w.fwd;
     // dk: the state is R^T [Dv, Dk]
@@ -219,7 +220,7 @@ int deer_linattn_adjoint(const deer_linattn_shape *s, int B, int T, const deer_v
     ro[1].Kd = Dv, ro[1].N = Dk;
     ro[1].reverse = true;
     ro[1].sc_kv = s->scale, ro[1].sc_o = 1.f;
-    ro[1].out = shared ? (void *)w.dk : dk, ro[1].out_f32 = shared, ro[1].wide_out = wide_out(dk, s->dtype, Dk);
+    ro[1].out = shared ? (void *)w.dk : dk, ro[1].out_f32 = shared, ro[1].wide_out = wide_out(ro[1].out, Dk);
     ro[1].init = g_state, ro[1].init_d = 1, ro[1].init_n = Dv;
     if (decay) ro[1].partner = vk, ro[1].dot = w.dk_dot, ro[1].anchor = w.rev;
     // dv: the state is R [Dk, Dv]
@@ -227,7 +228,7 @@ int deer_linattn_adjoint(const deer_linattn_shape *s, int B, int T, const deer_v
     ro[2].Kd = Dk, ro[2].N = Dv;
     ro[2].reverse = true;
     ro[2].sc_kv = s->scale, ro[2].sc_o = 1.f;
-    ro[2].out = dv, ro[2].wide_out = wide_out(dv, s->dtype, Dv);
+    ro[2].out = dv, ro[2].wide_out = wide_out(dv, Dv);
     ro[2].init = g_state, ro[2].init_d = Dv, ro[2].init_n = 1;
     ro[2].fin = dstate0, ro[2].fin_d = Dv, ro[2].fin_n = 1;
     const LinArgs a = args_of(s, B, T, DEER_OP_ADJOINT, log_decay, lengths);

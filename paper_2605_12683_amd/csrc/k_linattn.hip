@@ -17,37 +17,57 @@ namespace deer {
 // each (one pass over the segments, in place), and the walks proper start from there, all at once.
 // That reads k and v twice.
 
-// one element of one head's state per thread, the segments in the walk's order
+// four elements of one head's state per thread, the segments in the walk's order, eight of them
+// loaded at a time (32 heads of 128 x 128, 16 segments: 64 MB at the caches' rate)
 __global__ __launch_bounds__(256) void k_lin_join(LinArgs a, LinRoles rs) {
     const LinRole &ro = rs.r[blockIdx.y];
-    const int mat = ro.Kd * ro.N, per = (mat + 255) / 256;
-    const int bh = blockIdx.x / per, e = blockIdx.x % per * 256 + threadIdx.x;
+    const int mat = ro.Kd * ro.N, per = (mat + 1023) / 1024;
+    const int bh = blockIdx.x / per, e = (blockIdx.x % per * 256 + threadIdx.x) * 4;
     if (bh >= a.B * a.H || e >= mat) return;
-    const int b = bh / a.H, h = bh % a.H, d = e / ro.N, n = e % ro.N;
-    float S = ro.init ? ro.init[(size_t)bh * mat + (size_t)d * ro.init_d + (size_t)n * ro.init_n] : 0.f;
+    const int b = bh / a.H, h = bh % a.H, left = mat - e < 4 ? mat - e : 4;
+    const bool four = mat % 4 == 0;
+    float S[4] = {0.f, 0.f, 0.f, 0.f};
+    if (ro.init)
+        for (int r = 0; r < left; ++r) {
+            const int d = (e + r) / ro.N, n = (e + r) % ro.N;
+            S[r] = ro.init[(size_t)bh * mat + (size_t)d * ro.init_d + (size_t)n * ro.init_n];
+        }
     float *seg = ro.seg + (size_t)bh * a.nseg * mat + e;
     const float *dec = ro.seg_decay + (size_t)bh * a.nseg;
     constexpr int U = 8;
     for (int i0 = 0; i0 < a.nseg; i0 += U) {
-        float x[U], f[U];
+        float x[U][4], f[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int i = i0 + u, s = ro.reverse ? a.nseg - 1 - i : i;
             const bool on = i < a.nseg - 1 || (i == a.nseg - 1 && ro.fin);
-            x[u] = on ? seg[(size_t)s * mat] : 0.f;
+            const float *p = seg + (size_t)s * mat;
+            v4f y = {0.f, 0.f, 0.f, 0.f};
+            if (on && four) y = *(const v4f *)p;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[u][r] = y[r];
+            if (on && !four)
+                for (int r = 0; r < left; ++r) x[u][r] = p[r];
             f[u] = on ? dec[s] : 0.f;
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int i = i0 + u, s = ro.reverse ? a.nseg - 1 - i : i;
             if (i >= a.nseg) break;
-            seg[(size_t)s * mat] = S;
-            S = fmaf(f[u], S, x[u]);
+            float *p = seg + (size_t)s * mat;
+            if (four) *(v4f *)p = v4f{S[0], S[1], S[2], S[3]};
+            else
+                for (int r = 0; r < left; ++r) p[r] = S[r];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) S[r] = fmaf(f[u], S[r], x[u][r]);
         }
     }
     if (!ro.fin) return;
     const float f = ro.reverse ? __builtin_amdgcn_exp2f((float)gate_of(gate_raw(a, b, h, -1, length_of(a, b), true))) : 1.f;
-    ro.fin[(size_t)bh * mat + (size_t)d * ro.fin_d + (size_t)n * ro.fin_n] = f * S;
+    for (int r = 0; r < left; ++r) {
+        const int d = (e + r) / ro.N, n = (e + r) % ro.N;
+        ro.fin[(size_t)bh * mat + (size_t)d * ro.fin_d + (size_t)n * ro.fin_n] = f * S[r];
+    }
 }
 
 int launch_lin_join(const LinArgs &a, const LinRole *roles, int nroles, hipStream_t st) {
@@ -55,7 +75,7 @@ int launch_lin_join(const LinArgs &a, const LinRole *roles, int nroles, hipStrea
     int most = 0;
     for (int i = 0; i < nroles; ++i) {
         rs.r[i] = roles[i];
-        const int n = (roles[i].Kd * roles[i].N + 255) / 256;
+        const int n = (roles[i].Kd * roles[i].N + 1023) / 1024;
         most = n > most ? n : most;
     }
     KTimer kt("k_lin_join", st);
@@ -65,14 +85,12 @@ int launch_lin_join(const LinArgs &a, const LinRole *roles, int nroles, hipStrea
 }
 
 int lin_tiles(int Kd, int N) {
-    const int nb = 16 * nw_of(kt_of(Kd), N);
+    const int nb = nb_of(kt_of(Kd), N);
     return (N + nb - 1) / nb;
 }
 
-int lin_waves(int Kd, int N) { return lin_tiles(Kd, N) * nw_of(kt_of(Kd), N); }
-
 bool lin_same_tile(int Kd, int N, int Kd2, int N2) {
-    return kt_of(Kd) == kt_of(Kd2) && nw_of(kt_of(Kd), N) == nw_of(kt_of(Kd2), N2);
+    return kt_of(Kd) == kt_of(Kd2) && nb_of(kt_of(Kd), N) == nb_of(kt_of(Kd2), N2);
 }
 
 int launch_lin_walk(const LinArgs &a, const LinRole *roles, int nroles, bool states, bool dots, hipStream_t st) {
@@ -103,7 +121,16 @@ __global__ __launch_bounds__(kSpanThreads) void k_lin_decay_grad(LinArgs a, cons
     t1 = t1 < a.T ? t1 : a.T;
     double z = 0.0;
     const float *S = fwd + ((size_t)bh * na + sp) * elems, *R = rev + ((size_t)bh * na + sp) * elems;
-    for (int i = tid; i < elems; i += kSpanThreads) z += (double)S[i] * (double)R[i];
+    if (elems % 4 == 0) {
+        const v4f *S4 = (const v4f *)S, *R4 = (const v4f *)R;
+#pragma unroll 8
+        for (int i = tid; i < elems / 4; i += kSpanThreads) {
+            const v4f s = S4[i], r = R4[i];
+            z += ((double)s[0] * r[0] + (double)s[1] * r[1]) + ((double)s[2] * r[2] + (double)s[3] * r[3]);
+        }
+    } else {
+        for (int i = tid; i < elems; i += kSpanThreads) z += (double)S[i] * (double)R[i];
+    }
     sh[tid] = z;
     __syncthreads();
     for (int n = kSpanThreads / 2; n > 0; n >>= 1) {

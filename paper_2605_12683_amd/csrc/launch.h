@@ -349,7 +349,7 @@ struct LinRole {
     LinView partner;            // N wide, or p = null: dot[b, h, t] = <partner row, out row>
     float *dot;                 // [tiles][B, H, T]
     float *anchor;              // [B, H, anchors][Kd, N] or null: the state at every kLinAnchor steps
-    bool wide_out;              // out takes stores of four elements
+    bool wide_out;              // N is a multiple of 8 and out lies on 16 bytes
     // walks in segments: first what each segment adds by itself, then (joined) the state entering
     // each: [B, H, segments] matrices, element (d, n) at d seg_d + n seg_n, and the segments' decays
     float *seg, *seg_decay;
@@ -364,7 +364,6 @@ struct LinArgs {
     int seg_steps, nseg;        // segments of seg_steps steps (a multiple of 64), or one of all T
 };
 int lin_tiles(int Kd, int N);   // blocks that share the N columns of one head's state
-int lin_waves(int Kd, int N);              // their waves
 bool lin_same_tile(int Kd, int N, int Kd2, int N2);
 // all roles of one call have the same tile shape; states: what each segment adds (into seg,
 // seg_decay), else the outputs; dots: and dot, anchor (which are summed over many steps, so the

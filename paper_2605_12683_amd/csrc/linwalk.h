@@ -14,8 +14,8 @@
 // bits, for 16-bit outputs, 2^8 times finer than their own rounding; three: float32's 24) and always
 // into three where it enters the state, which is float32 for as long as the sequence lasts.
 //
-// One block of NW waves walks one head's chunks for 16 NW columns of the state; a wave keeps its 16
-// columns in registers for the whole walk, as matrix-core accumulators.  Their lane layout
+// One block of NW waves walks one head's chunks for NB = 16 NW CT columns of the state; a wave keeps
+// its 16 CT columns in registers for the whole walk, as matrix-core accumulators.  Their lane layout
 // (rows 4 g + r, column c of lane 16 g + c) is also that of an operand with the rows as the summed
 // index, if the other operand lists them in the order 4 g + 0..3, 16 + 4 g + 0..3 of each 32: q is
 // stored in LDS in that order, and the state enters its product with no exchange between lanes.  k
@@ -71,20 +71,21 @@ struct InParts<F16> { static constexpr int n = 2; };
 template <>
 struct InParts<F32> { static constexpr int n = 3; };
 
-// padded width of the summed side, and waves of 16 columns per block: eight where the columns fill
-// more than half of them and the state leaves the registers for four waves a SIMD (Kd <= 128)
+// padded width of the summed side, and columns of the state per block: 128 where they fill more than
+// half of them and Kd <= 128, else 64.  A block has four waves of 32 or 16 columns; eight of 16 for
+// float32 tiles of 128 x 128, whose LDS leaves room for one block only.
 constexpr int kt_of(int Kd) { return Kd <= 32 ? 32 : Kd <= 64 ? 64 : Kd <= 128 ? 128 : 256; }
-constexpr int nw_of(int KT, int N) { return N > 64 && KT <= 128 ? 8 : 4; }
+constexpr int nb_of(int KT, int N) { return N > 64 && KT <= 128 ? 128 : 64; }
 
 // what a walk leaves: the state that each segment adds by itself, from zero, and its decay; the
 // outputs (and the last state) from the state entering each segment; and with them the dots and the
 // states at the anchors
 enum { kStates = 0, kOut = 1, kOutDots = 2 };
 
-template <int NPI, int KT, int NW, int NPX, int MODE>
+template <int NPI, int KT, int NW, int CT, int NPX, int MODE>   // waves, 16-column tiles per wave
 struct LinTile {
     static constexpr bool OUT = MODE != kStates;
-    static constexpr int NB = 16 * NW, TH = 64 * NW;
+    static constexpr int NB = 16 * NW * CT, TH = 64 * NW;
     static constexpr int PQ = KT + 8, PK = KT + 16, PV = NB + 16;   // LDS row pitches: no bank conflicts
     static constexpr int pairs(int C) { return C == 64 ? 6 : 2; }   // (16 outputs, 32 sources) not all above the diagonal
     static constexpr int bytes(int C) {
@@ -94,7 +95,8 @@ struct LinTile {
     static constexpr int C = bytes(64) <= 80 * 1024 ? 64 : 32;
     static constexpr int lds = bytes(C);
     static constexpr int fit = 160 * 1024 / lds * NW / 4;
-    static constexpr int waves = fit > 4 ? 4 : fit;                 // per SIMD
+    static constexpr int most = OUT && (CT == 2 || KT == 256) ? 2 : CT == 2 || KT == 256 ? 3 : 4;   // (registers)
+    static constexpr int waves = fit > most ? most : fit;           // per SIMD
 };
 
 struct LinRoles {
@@ -124,38 +126,40 @@ template <class Ty, int C, int W, int TH>
 struct RowTile {
     using T = typename Ty::T;
     static constexpr int E = 16 / sizeof(T), UPR = W / E, NU = (C * UPR + TH - 1) / TH, ROWS = TH / UPR;
-    const T *base;
-    int st, col0, width;           // st in bytes
+    const char *base;              // of the next chunk
+    int st, col0, width, step;     // st, step in bytes
+    int off;                       // of the first unit
     bool fast, rev;
     v4u u[NU];
 
-    __device__ __forceinline__ void init(const LinView &x, int b, int h, int col0_, int width_, bool rev_) {
-        base = (const T *)x.p + b * x.sb + (h / x.r) * x.sh;
+    __device__ __forceinline__ void init(const LinView &x, int b, int h, int col0_, int width_, bool rev_, int t0) {
+        base = (const char *)((const T *)x.p + b * x.sb + (h / x.r) * x.sh + t0 * x.st);
         st = (int)(x.st * (long)sizeof(T)), col0 = col0_, width = width_, rev = rev_;
+        step = rev ? -ROWS * st : ROWS * st;
+        const int row = threadIdx.x / UPR, d = col0 + threadIdx.x % UPR * E;
+        off = d < width && row < C ? (rev ? C - 1 - row : row) * st + d * (int)sizeof(T) : (int)kOutside;
         fast = (((uintptr_t)base | (uintptr_t)st) & 15) == 0 && width % E == 0 && x.st >= width;
     }
 
-    __device__ __forceinline__ void load(int t0, int len) {
-        const int rows = len - t0 < C ? len - t0 : C;
-        const auto rs = bounded_rsrc((const char *)base + (long)t0 * st,
-                                     rows > 0 ? (uint32_t)((rows - 1) * st + width * (int)sizeof(T)) : 0u);
-        const int tid = afresh((int)threadIdx.x), r0 = tid / UPR, d = col0 + (tid % UPR) * E;
-        const int step = rev ? -ROWS * st : ROWS * st;
-        const uint32_t o = d < width && r0 < C ? (uint32_t)((rev ? C - 1 - r0 : r0) * st + d * (int)sizeof(T)) : kOutside;
+    __device__ __forceinline__ void load(int rows) {           // rows: how many exist, any number below 1 for none
+        const auto rs = bounded_rsrc(base, rows > 0 ? (uint32_t)((rows - 1) * st + width * (int)sizeof(T)) : 0u);
+        base += (long)(rev ? -C : C) * st;
+        const int o = afresh(off);
         if (fast) {
 #pragma unroll
             for (int i = 0; i < NU; ++i)
-                u[i] = __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)(o + (uint32_t)(i * step)), 0, 0));
+                u[i] = __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(rs, o + i * step, 0, 0));
             return;
         }
+        const int tid = afresh((int)threadIdx.x), d = col0 + tid % UPR * E;
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
-            const int row = i * ROWS + r0, j = rev ? C - 1 - row : row;
+            const int row = i * ROWS + tid / UPR, j = rev ? C - 1 - row : row;
             const bool on = row < C && j < rows;
             uint32_t x[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const int at = on && d + e < width ? (int)(o + (uint32_t)(i * step) + e * sizeof(T)) : (int)kOutside;
+                const int at = on && d + e < width ? o + i * step + e * (int)sizeof(T) : (int)kOutside;
                 if constexpr (sizeof(T) == 4) x[e] = bload_u(rs, (uint32_t)at, 0);
                 else x[e] = __builtin_bit_cast(uint16_t, __builtin_amdgcn_raw_buffer_load_b16(rs, at, 0, 0));
             }
@@ -211,9 +215,9 @@ struct RowTile {
     }
 };
 
-// four rows of one column: lane 16 g + c of a wave gets rows row0 + 4 g + 0..3 of column col0 + c
-__device__ __forceinline__ v2u read_turned(const uint16_t *lds, int pitch, int row0, int col0, int g, int c) {
-    const uint16_t *p = lds + (row0 + 4 * g + (c >> 2)) * pitch + col0 + 4 * (c & 3);
+// LDS rows read across: each group of 16 lanes (4 rows x 4 lanes, lane 4 i + j at columns 4 j + 0..3 of
+// row i, p its own address) gets 16 columns, lane c the four rows' elements of column c
+__device__ __forceinline__ v2u read_turned(const uint16_t *p) {
     return __builtin_bit_cast(
         v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)p));
 }
@@ -249,13 +253,30 @@ __device__ __forceinline__ v4f mfma_parts(const v4u (&x)[NA], const v4u (&y)[NB]
     return acc;
 }
 
+// the same of every pair of X and Y operands, acc(x, y) += x y, so that consecutive products belong
+// to different sums
+template <int LIM, int X, int Y, int NA, int NB, class Acc>
+__device__ __forceinline__ void mfma_block(const v4u (&x)[X][NA], const v4u (&y)[Y][NB], Acc acc) {
+#pragma unroll
+    for (int s = LIM; s >= 0; --s)
+#pragma unroll
+        for (int p = 0; p < NA; ++p) {
+            const int q = s - p;
+            if (q < 0 || q >= NB) continue;
+#pragma unroll
+            for (int i = 0; i < X; ++i)
+#pragma unroll
+                for (int j = 0; j < Y; ++j) acc(i, j) = mfma_b(x[i][p], y[j][q], acc(i, j));
+        }
+}
+
 // ---- decays of a chunk --------------------------------------------------------------------------
 
 template <int C>
 struct Decays {
     float hi[C], lo[C];   // log2 decay summed up to each step
     float into[C];        // sc_kv exp2(L - c): what a step's k v^T has left at the chunk's end
-    float from[C];        // exp2(c): what the entering state has left at each step
+    float from[C];        // sc_o exp2(c): what the entering state has left at each step
     float all;            // exp2(L)
     float pad[3];
 };
@@ -271,7 +292,7 @@ __device__ __forceinline__ double dpp_or_zero(double x) {
 
 // by one wave; raw: this lane's log decay (C = 32: the upper half wave repeats the lower).  Returns L.
 template <int C>
-__device__ __forceinline__ double chunk_decays(Decays<C> &d, float raw, float sc_kv) {
+__device__ __forceinline__ double chunk_decays(Decays<C> &d, float raw, float sc_kv, float sc_o) {
     const int lane = threadIdx.x & 63, i = lane & (C - 1);
     double s = gate_of(raw);
     s += dpp_or_zero<0x111, 15>(s);        // row_shr: lanes of each 16
@@ -288,26 +309,26 @@ __device__ __forceinline__ double chunk_decays(Decays<C> &d, float raw, float sc
     d.hi[i] = hi;
     d.lo[i] = (float)(s - (double)hi);
     d.into[i] = sc_kv * __builtin_amdgcn_exp2f((float)(L - s));
-    d.from[i] = __builtin_amdgcn_exp2f(hi);
+    d.from[i] = sc_o * __builtin_amdgcn_exp2f(hi);
     if (i == 0) d.all = __builtin_amdgcn_exp2f((float)L);
     return L;
 }
 
 // ---- the walk ---------------------------------------------------------------------------------
 
-template <class Ty, int KT, int NW, int NPX, int MODE>
-__global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, NPX, MODE>::waves)) void k_lin_walk(LinArgs a,
-                                                                                                          LinRoles rs) {
+template <class Ty, int KT, int NW, int CT, int NPX, int MODE>
+__global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, MODE>::waves)) void k_lin_walk(LinArgs a,
+                                                                                                              LinRoles rs) {
     constexpr int NPI = InParts<Ty>::n;
-    using Tile = LinTile<NPI, KT, NW, NPX, MODE>;
+    using Tile = LinTile<NPI, KT, NW, CT, NPX, MODE>;
     using T = typename Ty::T;
     constexpr bool OUT = Tile::OUT, DOTS = MODE == kOutDots;
     constexpr int C = Tile::C, NB = Tile::NB, TH = Tile::TH, PQ = Tile::PQ, PK = Tile::PK, PV = Tile::PV;
     constexpr int NT = C / 16, KS = C / 32, DT = KT / 16;
-    // operands read from LDS at a time: as many as the registers hold twice (dividing NT, DT)
-    constexpr bool TIGHT = KT == 128 && NW == 8;
+    // operands read from LDS at a time: as many as the registers hold twice (dividing KT / 32, NT, DT)
+    constexpr bool TIGHT = KT == 128 && Tile::waves == 4;
     constexpr int UB = TIGHT && DOTS ? 1 : KT / 32 * NPI <= 4 ? KT / 32 : NPI == 1 ? 4 : NPI == 2 ? 2 : 1;
-    constexpr int QB = TIGHT ? 2 : NT, KB = NPI == 1 && !TIGHT && DT > 2 ? 4 : 2, PB = NPX == 2 && !TIGHT ? 2 : 1;
+    constexpr int QB = TIGHT || CT == 2 || KT == 256 ? 2 : NT, KB = NPI == 1 && !TIGHT && DT > 2 ? 4 : 2, PB = NPX == 2 && !TIGHT ? 2 : 1;
     extern __shared__ __align__(16) unsigned char smem[];
     uint16_t *Ks = (uint16_t *)smem, *Vs = Ks + NPI * C * PK, *Qs = Vs + NPI * C * PV;
     unsigned char *rest = (unsigned char *)(Qs + (OUT ? NPI * C * PQ : 0));
@@ -323,29 +344,31 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, NPX, MODE
     if ((long)blockIdx.x >= units) return;
     const int tile = blockIdx.x % tiles, seg = blockIdx.x / tiles % a.nseg, bh = blockIdx.x / tiles / a.nseg;
     const int b = bh / a.H, h = bh % a.H;
-    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // the lane, found anew in each phase: what depends on it takes no registers in the others
+    auto lane_now = [] { return afresh((int)threadIdx.x) & 63; };
     const bool rev = ro.reverse;
     const int len = length_of(a, b);
     const int lo = seg * a.seg_steps, hi = lo + a.seg_steps < a.T ? lo + a.seg_steps : a.T;
     const int chunks = (hi - lo + C - 1) / C;
     const int Kd = ro.Kd, N = ro.N;
     const size_t mat = (size_t)Kd * N;
-    const int col0 = tile * NB, n0 = col0 + w * 16;            // the block's and the wave's first column
+    const int col0 = tile * NB, n0 = col0 + w * 16 * CT;       // the block's and the wave's first column
 
     // the segment that comes last adds to no other: its own sum is needed for the last state only
     if (!OUT && seg == (rev ? 0 : a.nseg - 1) && !ro.fin) return;
 
+    auto t0_of = [&](int n) { return lo + (rev ? chunks - 1 - n : n) * C; };
     RowTile<Ty, C, KT, TH> qr, kr;
     RowTile<Ty, C, NB, TH> vr;
-    kr.init(ro.k, b, h, 0, Kd, rev);
-    vr.init(ro.v, b, h, col0, N, rev);
-    if constexpr (OUT) qr.init(ro.q, b, h, 0, Kd, rev);
-    auto t0_of = [&](int n) { return lo + (rev ? chunks - 1 - n : n) * C; };
-    auto load = [&](int n) {
-        const int t0 = t0_of(n);
-        kr.load(t0, len);
-        vr.load(t0, len);
-        if constexpr (OUT) qr.load(t0, len);
+    kr.init(ro.k, b, h, 0, Kd, rev, t0_of(0));
+    vr.init(ro.v, b, h, col0, N, rev, t0_of(0));
+    if constexpr (OUT) qr.init(ro.q, b, h, 0, Kd, rev, t0_of(0));
+    auto load = [&](int n) {                                   // of one chunk after the other
+        const int left = len - t0_of(n), rows = left < C ? left : C;
+        kr.load(rows);
+        vr.load(rows);
+        if constexpr (OUT) qr.load(rows);
     };
     auto gate = [&](int n) {
         if (n >= chunks) return 0.f;
@@ -353,10 +376,13 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, NPX, MODE
         return gate_raw(a, b, h, t0_of(n) + (rev ? C - 1 - i : i), len, rev);
     };
 
+    // Column c of the wave's tile ct is column n0 + col(c, ct): with two tiles a lane's four outputs
+    // of both are eight columns in a row.
+    auto col = [](int c, int ct) { return CT == 2 ? 8 * (c >> 2) + 4 * ct + (c & 3) : c; };
     // element (d, n) of a matrix of Kd N floats, beyond its rows and columns outside
-    v4f S[DT];
-    auto at = [&](int l, int dt, int r, int sd, int sn) {
-        const int d = dt * 16 + 4 * (l >> 4) + r, n = n0 + (l & 15);
+    v4f S[DT][CT];
+    auto at = [&](int l, int dt, int ct, int r, int sd, int sn) {
+        const int d = dt * 16 + 4 * (l >> 4) + r, n = n0 + col(l & 15, ct);
         return d < Kd && n < N ? (uint32_t)(d * sd + n * sn) * 4u : kOutside;
     };
     {
@@ -367,10 +393,13 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, NPX, MODE
             else if (ro.init) src = ro.init + bh * mat, sd = ro.init_d, sn = ro.init_n;
         }
         const auto rsrc = bounded_rsrc(src, src ? (uint32_t)(mat * 4) : 0u);
+        const int l = threadIdx.x & 63;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) S[dt][r] = bload(rsrc, at(lane, dt, r, sd, sn), 0);
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) S[dt][ct][r] = bload(rsrc, at(l, dt, ct, r, sd, sn), 0);
     }
     auto put_state = [&](float *dst, int sd, int sn, float f) {
         const auto rsrc = bounded_rsrc(dst, (uint32_t)(mat * 4));
@@ -378,24 +407,26 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, NPX, MODE
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    bstore_u(rsrc, __float_as_uint(f * S[dt][r]), at(l, dt, r, sd, sn), 0);
+                    bstore_u(rsrc, __float_as_uint(f * S[dt][ct][r]), at(l, dt, ct, r, sd, sn), 0);
                     if (r == 3) __builtin_amdgcn_sched_barrier(0);
                 }
     };
 
-    // this lane's part of the outputs: step i = 16 it + c of a chunk, columns n0 + 4 g + 0..3
+    // this lane's part of the outputs: step i = 16 it + c of a chunk, columns n0 + 4 CT g + 0 .. 4 CT - 1
     const int out_size = ro.out_f32 ? 4 : (int)sizeof(T), out_row = a.H * N * out_size;   // C rows below 2^31 bytes
-    auto out_off = [&](int l, int it, int row, int size) {
-        const int i = it * 16 + (l & 15), n = n0 + 4 * (l >> 4);
-        return n < N ? (uint32_t)((rev ? C - 1 - i : i) * row + n * size) : kOutside;
+    auto out_off = [&](int l, int row, int size) {             // of it = 0; the others 16 rows further each
+        const int n = n0 + 4 * CT * (l >> 4);
+        return n < N ? (rev ? C - 1 - (l & 15) : l & 15) * row + n * size : (int)kOutside;
     };
     const T *partner = nullptr;
     bool partner_fast = false;
     if constexpr (DOTS) {
         partner = (const T *)ro.partner.p + b * ro.partner.sb + (h / ro.partner.r) * ro.partner.sh;
         const long row = ro.partner.st * (long)sizeof(T);
-        partner_fast = (((uintptr_t)partner | (uintptr_t)row) & (4 * sizeof(T) - 1)) == 0 && N % 4 == 0 &&
+        partner_fast = (((uintptr_t)partner | (uintptr_t)row) & (4 * CT * sizeof(T) - 1) & 15) == 0 && N % (4 * CT) == 0 &&
                        ro.partner.st >= N;
     }
 
@@ -411,12 +442,12 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, NPX, MODE
     double total = 0.0;                                        // last wave: log2 decay of the segment
     float raw = 0.f;
     if (w == NW - 1) {
-        const double L = chunk_decays<C>(dec[0], gate(0), ro.sc_kv);
+        const double L = chunk_decays<C>(dec[0], gate(0), ro.sc_kv, ro.sc_o);
         if (!OUT) total += L;
         raw = __int_as_float(afresh(__float_as_int(gate(1))));
     }
     const int na = (a.T + kLinAnchor - 1) / kLinAnchor;
-
+    const float sc_p = ro.sc_kv * ro.sc_o;
     store();
 
     // The next chunk's rows are loaded while this one is computed and go to LDS before this one's
@@ -430,7 +461,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, NPX, MODE
             if (w == NW - 1) raw = gate(n + 2);
             load(n + 1);
             if (w == NW - 1) {
-                const double L = chunk_decays<C>(dec[(n + 1) & 1], next, ro.sc_kv);
+                const double L = chunk_decays<C>(dec[(n + 1) & 1], next, ro.sc_kv, ro.sc_o);
                 if (!OUT) total += L;
             }
         }
@@ -441,18 +472,18 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, NPX, MODE
         }
         __builtin_amdgcn_sched_barrier(0);
 
-        v4f O[NT];
+        v4f O[NT][CT];
         if constexpr (OUT) {
             // decayed scores, transposed: rows j, columns i
             for (int tl = w; tl < NT * (NT + 1) / 2; tl += NW) {
-                const int lane = afresh((int)threadIdx.x) & 63, g = lane >> 4, c = lane & 15;
+                const int lane = lane_now(), g = lane >> 4, c = lane & 15;
                 const int it = tl >= 6 ? 3 : tl >= 3 ? 2 : tl >= 1 ? 1 : 0, jt = tl - it * (it + 1) / 2;
                 const int i = it * 16 + c, j0 = jt * 16 + 4 * g;
                 const float hi_i = dc.hi[i], lo_i = dc.lo[i];
                 const v4f hi_j = *(const v4f *)(dc.hi + j0), lo_j = *(const v4f *)(dc.lo + j0);
                 v4f acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int u0 = 0; u0 < KT / 32; u0 += UB) {   // reads of UB products at a time
+                for (int u0 = 0; u0 < KT / 32; u0 += UB) {
                     v4u kf[UB][NPI], qf[UB][NPI];
 #pragma unroll
                     for (int u = 0; u < UB; ++u)
@@ -471,7 +502,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, NPX, MODE
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const float e = (hi_i - hi_j[r]) + (lo_i - lo_j[r]);
-                    const float p = acc[r] * ro.sc_kv * __builtin_amdgcn_exp2f(e);
+                    const float p = acc[r] * sc_p * __builtin_amdgcn_exp2f(e);
                     x[r] = j0 + r <= i ? p : 0.f;
                 }
                 uint32_t *dst = (uint32_t *)(Ps + pair(it, jt >> 1) * NPX * 64 + lane) + (jt & 1) * 2;
@@ -482,9 +513,11 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, NPX, MODE
                 for (int q = 0; q < NPX; ++q) *(v2u *)(dst + q * 64 * 4) = v2u{p0[q], p1[q]};
             }
             // what the entering state gives, transposed: rows n, columns i
-            const int lane = afresh((int)threadIdx.x) & 63, g = lane >> 4, c = lane & 15;
+            const int lane = lane_now(), g = lane >> 4, c = lane & 15;
 #pragma unroll
-            for (int it = 0; it < NT; ++it) O[it] = v4f{0.f, 0.f, 0.f, 0.f};
+            for (int it = 0; it < NT; ++it)
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) O[it][ct] = v4f{0.f, 0.f, 0.f, 0.f};
             v4u qf[2][QB][NPI];   // read QB at a time, one time ahead
             auto read_q = [&](int n) {
                 const int u = n / (NT / QB), it0 = n % (NT / QB) * QB;
@@ -496,91 +529,91 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, NPX, MODE
             };
             constexpr int QN = KT / 32 * (NT / QB);
             read_q(0);
-            v4u sf[NPX];
+            v4u sf[CT][NPX];
 #pragma unroll
             for (int n = 0; n < QN; ++n) {
                 const int u = n / (NT / QB), it0 = n % (NT / QB) * QB;
                 if (n + 1 < QN) read_q(n + 1);
                 __builtin_amdgcn_sched_barrier(0);
-                if (it0 == 0) {
-                    float x[8];
+                if (it0 == 0)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) x[r] = S[2 * u][r], x[4 + r] = S[2 * u + 1][r];
-                    split8<NPX>(x, sf);
-                }
+                    for (int ct = 0; ct < CT; ++ct) {
+                        float x[8];
 #pragma unroll
-                for (int m = 0; m < QB; ++m) O[it0 + m] = mfma_parts<NPX - 1>(sf, qf[n & 1][m], O[it0 + m]);
+                        for (int r = 0; r < 4; ++r) x[r] = S[2 * u][ct][r], x[4 + r] = S[2 * u + 1][ct][r];
+                        split8<NPX>(x, sf[ct]);
+                    }
+                mfma_block<NPX - 1, CT, QB>(sf, qf[n & 1], [&](int ct, int m) -> v4f & { return O[it0 + m][ct]; });
                 __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
-            for (int it = 0; it < NT; ++it) O[it] *= dc.from[it * 16 + c];
+            for (int it = 0; it < NT; ++it) {
+                const float f = dc.from[it * 16 + c];
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) O[it][ct] *= f;
+            }
             lds_barrier();
         }
 
-        typedef T v4t __attribute__((ext_vector_type(4)));
-        v4t pr[DOTS ? NT : 1];        // the partner's rows, used at the end
+        constexpr int PW = 4 * CT * sizeof(T) / 4 < 4 ? 1 : CT * sizeof(T) / 4;   // 16-byte words of a partner row
+        v4u pr[DOTS ? NT : 1][PW];    // the partner's rows, used at the end
         auto read_partner = [&] {
             const int rows = len - t0 < C ? len - t0 : C;
             const auto prs = bounded_rsrc(partner + t0 * ro.partner.st,
                                           rows > 0 ? (uint32_t)(((rows - 1) * ro.partner.st + N) * sizeof(T)) : 0u);
             const int row = (int)(ro.partner.st * (long)sizeof(T)), l = afresh((int)threadIdx.x) & 63;
+            const int off0 = out_off(l, row, sizeof(T));
 #pragma unroll
             for (int it = 0; it < NT; ++it) {
-                const int off = (int)out_off(l, it, row, sizeof(T));
+                const int off = off0 + (rev ? -16 * it : 16 * it) * row;
                 if (partner_fast) {
-                    if constexpr (sizeof(T) == 4)
-                        pr[it] = __builtin_bit_cast(v4t, __builtin_amdgcn_raw_buffer_load_b128(prs, off, 0, 0));
-                    else
-                        pr[it] = __builtin_bit_cast(v4t, __builtin_amdgcn_raw_buffer_load_b64(prs, off, 0, 0));
+                    if constexpr (4 * CT * sizeof(T) == 8) {
+                        const v2u x = __builtin_bit_cast(v2u, __builtin_amdgcn_raw_buffer_load_b64(prs, off, 0, 0));
+                        pr[it][0] = v4u{x[0], x[1], 0, 0};
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < PW; ++k)
+                            pr[it][k] = __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(prs, off + 16 * k, 0, 0));
+                    }
                     continue;
                 }
-                const int i = it * 16 + (l & 15), j = rev ? C - 1 - i : i, nn = n0 + 4 * (l >> 4);
+                const int i = it * 16 + (l & 15), j = rev ? C - 1 - i : i, nn = n0 + 4 * CT * (l >> 4);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int at = j < rows && nn + r < N ? off + r * (int)sizeof(T) : (int)kOutside;
+                for (int k = 0; k < PW; ++k) pr[it][k] = v4u{0, 0, 0, 0};
+#pragma unroll
+                for (int e = 0; e < 4 * CT; ++e) {
+                    const int p = j < rows && nn + e < N ? off + e * (int)sizeof(T) : (int)kOutside;
                     if constexpr (sizeof(T) == 4)
-                        pr[it][r] = bload(prs, (uint32_t)at, 0);
+                        pr[it][e / 4][e % 4] = bload_u(prs, (uint32_t)p, 0);
                     else
-                        pr[it][r] = __builtin_bit_cast(T, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(prs, at, 0, 0));
-                    __builtin_amdgcn_sched_barrier(0);
+                        pr[it][e / 8][e / 2 % 4] |= (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(prs, p, 0, 0)
+                                                    << (e & 1) * 16;
                 }
+                __builtin_amdgcn_sched_barrier(0);
             }
         };
 
         // the chunk's own steps, and the state at its end
         const float all = dc.all;
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) S[dt] *= all;
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) S[dt][ct] *= all;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-            const int lane = afresh((int)threadIdx.x) & 63, g = lane >> 4, c = lane & 15;
-            v4u vf[NPI], sv[3];
-            float x[8];
+            const int lane = lane_now(), g = lane >> 4, c = lane & 15;
+            v4u vf[CT][NPI], sv[CT][3];
+            const v4f into0 = *(const v4f *)(dc.into + ks * 32 + 4 * g), into1 = *(const v4f *)(dc.into + ks * 32 + 16 + 4 * g);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = 0.f;
+            for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-            for (int p = 0; p < NPI; ++p) {
-                const uint16_t *vp = Vs + p * C * PV;
-                const v2u v0 = read_turned(vp, PV, ks * 32, w * 16, g, c);
-                const v2u v1 = read_turned(vp, PV, ks * 32 + 16, w * 16, g, c);
-                vf[p] = v4u{v0[0], v0[1], v1[0], v1[1]};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    x[2 * e] += __uint_as_float(vf[p][e] << 16);
-                    x[2 * e + 1] += __uint_as_float(vf[p][e] & 0xffff0000u);
+                for (int p = 0; p < NPI; ++p) {
+                    const uint16_t *vp = Vs + p * C * PV + w * 16 * CT + (CT == 2 ? 8 * (c & 3) + 4 * ct : 4 * (c & 3));
+                    const v2u v0 = read_turned(vp + (ks * 32 + 4 * g + (c >> 2)) * PV);
+                    const v2u v1 = read_turned(vp + (ks * 32 + 16 + 4 * g + (c >> 2)) * PV);
+                    vf[ct][p] = v4u{v0[0], v0[1], v1[0], v1[1]};
                 }
-            }
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                x[r] *= dc.into[ks * 32 + 4 * g + r];
-                x[4 + r] *= dc.into[ks * 32 + 16 + 4 * g + r];
-            }
-            split8<3>(x, sv);
-
-            // products of the scores with v, then of k with the decayed v, KB of each at a time, the
-            // operands of the next ones read while these run
-            constexpr int PN = (NT + PB - 1) / PB;
-            v4u pf[2][PB][NPX], kf[2][KB][NPI];
+            v4u pf[2][PB][NPX], kf[2][KB][NPI];   // the operands of the next products read while these run
             auto read_p = [&](int n) {
 #pragma unroll
                 for (int m = 0; m < PB; ++m) {
@@ -595,29 +628,40 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, NPX, MODE
                 for (int m = 0; m < KB; ++m)
 #pragma unroll
                     for (int p = 0; p < NPI; ++p) {
-                        const uint16_t *kp = Ks + p * C * PK;
-                        const v2u k0 = read_turned(kp, PK, ks * 32, (n * KB + m) * 16, g, c);
-                        const v2u k1 = read_turned(kp, PK, ks * 32 + 16, (n * KB + m) * 16, g, c);
+                        const uint16_t *kp = Ks + p * C * PK + (ks * 32 + 4 * g + (c >> 2)) * PK + (n * KB + m) * 16 + 4 * (c & 3);
+                        const v2u k0 = read_turned(kp), k1 = read_turned(kp + 16 * PK);
                         kf[n & 1][m][p] = v4u{k0[0], k0[1], k1[0], k1[1]};
                     }
             };
+            if constexpr (OUT) read_p(0);
+            else read_k(0);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                float x[8];
+#pragma unroll
+                for (int p = 0; p < NPI; ++p)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float x0 = __uint_as_float(vf[ct][p][e] << 16), x1 = __uint_as_float(vf[ct][p][e] & 0xffff0000u);
+                        x[2 * e] = p ? x[2 * e] + x0 : x0;
+                        x[2 * e + 1] = p ? x[2 * e + 1] + x1 : x1;
+                    }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x[r] *= into0[r], x[4 + r] *= into1[r];
+                split8<3>(x, sv[ct]);
+            }
             if constexpr (OUT) {
-                read_p(0);
+                constexpr int PN = (NT + PB - 1) / PB;
 #pragma unroll
                 for (int n = 0; n < PN; ++n) {
                     if (2 * ks + n * PB >= NT) break;
                     if (2 * ks + (n + 1) * PB < NT) read_p(n + 1);
                     else read_k(0);
                     __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                    for (int m = 0; m < PB; ++m) {
-                        const int it = 2 * ks + n * PB + m;
-                        if (it < NT) O[it] = mfma_parts<NPX - 1>(vf, pf[n & 1][m], O[it]);
-                    }
+                    mfma_block<NPX - 1, CT, PB>(vf, pf[n & 1], [&](int ct, int m) -> v4f & { return O[2 * ks + n * PB + m][ct]; });
                     __builtin_amdgcn_sched_barrier(0);
                 }
-            } else {
-                read_k(0);
             }
             if constexpr (DOTS)
                 if (ks == KS - 1) read_partner();
@@ -625,63 +669,84 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, NPX, MODE
             for (int n = 0; n < DT / KB; ++n) {
                 if (n + 1 < DT / KB) read_k(n + 1);
                 __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int m = 0; m < KB; ++m) S[n * KB + m] = mfma_parts<2>(kf[n & 1][m], sv, S[n * KB + m]);
+                mfma_block<2, KB, CT>(kf[n & 1], sv, [&](int m, int ct) -> v4f & { return S[n * KB + m][ct]; });
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
 
-        __builtin_amdgcn_sched_barrier(0);
-        if constexpr (OUT) {
-            const int lane = afresh((int)threadIdx.x) & 63, g = lane >> 4, c = lane & 15;
-            const bool tail = t0 + C > len;      // some rows lie behind the sequence's end: zero
+        if constexpr (DOTS) {
+            const int lane = lane_now(), g = lane >> 4, c = lane & 15;
 #pragma unroll
             for (int it = 0; it < NT; ++it) {
-                const int i = it * 16 + c, j = rev ? C - 1 - i : i;
-                O[it] *= ro.sc_o;
-                if (tail && t0 + j >= len) O[it] = v4f{0.f, 0.f, 0.f, 0.f};
-                if constexpr (DOTS) {
-                    float dot = 0.f;
+                const int i = it * 16 + c;
+                float dot = 0.f;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) dot = fmaf(O[it][r], Ty::up(pr[it][r]), dot);
-                    dot = group_sum(dot);
-                    if (g == 0) dots[w * C + i] = dot;
+                for (int e = 0; e < 4 * CT; ++e) {
+                    float y;
+                    if constexpr (sizeof(T) == 4) {
+                        y = __uint_as_float(pr[it][e / 4][e % 4]);
+                    } else {
+                        const uint16_t u = (uint16_t)(pr[it][e / 8][e / 2 % 4] >> (e & 1) * 16);
+                        y = Ty::up(__builtin_bit_cast(T, u));
+                    }
+                    dot = fmaf(O[it][e / 4][e % 4], y, dot);
                 }
+                dot = group_sum(dot);
+                if (g == 0) dots[w * C + i] = t0 + (rev ? C - 1 - i : i) < len ? dot : 0.f;
             }
-        }
-        if constexpr (DOTS)
             if (anc && !rev) put_state(anc, N, 1, 1.f);
+        }
         lds_barrier();
         if (n + 1 < chunks) {
             store();
             raw = __int_as_float(afresh(__float_as_int(raw)));   // (loaded before the rows: no wait for it later)
         }
         if constexpr (OUT) {
+            const int l = lane_now();
+            if (t0 + C > len)             // rows behind the sequence's end: zero
+#pragma unroll
+                for (int it = 0; it < NT; ++it) {
+                    const int i = it * 16 + (l & 15);
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct)
+                        if (t0 + (rev ? C - 1 - i : i) >= len) O[it][ct] = v4f{0.f, 0.f, 0.f, 0.f};
+                }
             const int rows = a.T - t0 < C ? a.T - t0 : C;
             const size_t first = (((size_t)b * a.T + t0) * a.H + h) * N;
             const auto ors = bounded_rsrc((char *)ro.out + first * out_size,
                                           (uint32_t)((rows - 1) * out_row + N * out_size));
-            const int l = afresh((int)threadIdx.x) & 63;
+            const int off0 = out_off(l, out_row, out_size), step = (rev ? -16 : 16) * out_row;
+            if (ro.wide_out && (sizeof(T) == 4 || ro.out_f32)) {
 #pragma unroll
-            for (int it = 0; it < NT; ++it) {
-                const v4f o = O[it];
-                const int off = (int)out_off(l, it, out_row, out_size);
-                const bool four = sizeof(T) == 4 || ro.out_f32;
-                union { T x[4]; uint16_t h[4]; v2u u; } y;
-                if constexpr (sizeof(T) == 2)
-                    for (int r = 0; r < 4; ++r) y.x[r] = Ty::down(o[r]);
-                if (ro.wide_out) {
-                    if (four) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, o), ors, off, 0, 0);
-                    else __builtin_amdgcn_raw_buffer_store_b64(y.u, ors, off, 0, 0);
-                    continue;
-                }
-                const int nn = n0 + 4 * (l >> 4);
+                for (int it = 0; it < NT; ++it)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int at = nn + r < N ? off + r * out_size : (int)kOutside;
-                    if (four) bstore_u(ors, __float_as_uint(o[r]), (uint32_t)at, 0);
-                    else __builtin_amdgcn_raw_buffer_store_b16(y.h[r], ors, at, 0, 0);
+                    for (int ct = 0; ct < CT; ++ct)
+                        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, O[it][ct]), ors,
+                                                               off0 + it * step + ct * 16, 0, 0);
+            } else if (ro.wide_out) {
+#pragma unroll
+                for (int it = 0; it < NT; ++it) {
+                    union { T x[4 * CT]; v2u u; v4u v; } y;
+#pragma unroll
+                    for (int e = 0; e < 4 * CT; ++e) y.x[e] = Ty::down(O[it][e / 4][e % 4]);
+                    if constexpr (CT == 2) __builtin_amdgcn_raw_buffer_store_b128(y.v, ors, off0 + it * step, 0, 0);
+                    else __builtin_amdgcn_raw_buffer_store_b64(y.u, ors, off0 + it * step, 0, 0);
                 }
+            } else {
+                const int nn = n0 + 4 * CT * (l >> 4);
+#pragma unroll
+                for (int it = 0; it < NT; ++it)
+#pragma unroll
+                    for (int e = 0; e < 4 * CT; ++e) {
+                        const int p = nn + e < N ? off0 + it * step + e * out_size : (int)kOutside;
+                        const float o = O[it][e / 4][e % 4];
+                        if (sizeof(T) == 4 || ro.out_f32) {
+                            bstore_u(ors, __float_as_uint(o), (uint32_t)p, 0);
+                        } else if constexpr (sizeof(T) == 2) {
+                            __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, (T)Ty::down(o)), ors, p, 0, 0);
+                        }
+                        if (e == 4 * CT - 1) __builtin_amdgcn_sched_barrier(0);
+                    }
             }
         }
         if constexpr (DOTS) {
@@ -702,15 +767,16 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, NPX, MODE
         }
     } else {
         put_state(ro.seg + ((size_t)bh * a.nseg + seg) * mat, N, 1, 1.f);
-        if (w == NW - 1 && lane == 0 && tile == 0) ro.seg_decay[(size_t)bh * a.nseg + seg] = __builtin_amdgcn_exp2f((float)total);
+        if (w == NW - 1 && (threadIdx.x & 63) == 0 && tile == 0)
+            ro.seg_decay[(size_t)bh * a.nseg + seg] = __builtin_amdgcn_exp2f((float)total);
     }
 }
 
 // ---- launches -------------------------------------------------------------------------------------
 
-template <class Ty, int KT, int NW, int NPX, int MODE>
+template <class Ty, int KT, int NW, int CT, int NPX, int MODE>
 int launch_walk_tile(const LinArgs &a, const LinRole *roles, int n, hipStream_t st) {
-    using Tile = LinTile<InParts<Ty>::n, KT, NW, NPX, MODE>;
+    using Tile = LinTile<InParts<Ty>::n, KT, NW, CT, NPX, MODE>;
     LinRoles rs{};
     int tiles = 0;
     for (int i = 0; i < n; ++i) {
@@ -718,27 +784,29 @@ int launch_walk_tile(const LinArgs &a, const LinRole *roles, int n, hipStream_t 
         const int t = (roles[i].N + Tile::NB - 1) / Tile::NB;
         tiles = t > tiles ? t : tiles;
     }
-    const void *fn = (const void *)k_lin_walk<Ty, KT, NW, NPX, MODE>;
+    const void *fn = (const void *)k_lin_walk<Ty, KT, NW, CT, NPX, MODE>;
     if (Tile::lds > 64 * 1024) DEER_HIP(hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, Tile::lds));
     KTimer kt(MODE == kStates ? "k_lin_walk_states" : "k_lin_walk", st);
-    hipLaunchKernelGGL((k_lin_walk<Ty, KT, NW, NPX, MODE>), dim3((unsigned)(a.B * a.H * a.nseg * tiles), n), dim3(64 * NW),
-                       Tile::lds, st, a, rs);
+    hipLaunchKernelGGL((k_lin_walk<Ty, KT, NW, CT, NPX, MODE>), dim3((unsigned)(a.B * a.H * a.nseg * tiles), n),
+                       dim3(64 * NW), Tile::lds, st, a, rs);
     DEER_LAUNCH_CHECK("k_lin_walk");
     return DEER_OK;
 }
 
 template <class Ty, int NPX, int MODE>
 int launch_walk_parts(const LinArgs &a, const LinRole *roles, int n, hipStream_t st) {
-    const int KT = kt_of(roles[0].Kd), NW = nw_of(KT, roles[0].N);
-    if (KT == 256) return launch_walk_tile<Ty, 256, 4, NPX, MODE>(a, roles, n, st);
-    if (NW == 4) {
-        if (KT == 32) return launch_walk_tile<Ty, 32, 4, NPX, MODE>(a, roles, n, st);
-        if (KT == 64) return launch_walk_tile<Ty, 64, 4, NPX, MODE>(a, roles, n, st);
-        return launch_walk_tile<Ty, 128, 4, NPX, MODE>(a, roles, n, st);
+    constexpr int NPI = InParts<Ty>::n;
+    const int KT = kt_of(roles[0].Kd), nb = nb_of(KT, roles[0].N);
+    if (KT == 256) return launch_walk_tile<Ty, 256, 4, 1, NPX, MODE>(a, roles, n, st);
+    if (nb == 64) {
+        if (KT == 32) return launch_walk_tile<Ty, 32, 4, 1, NPX, MODE>(a, roles, n, st);
+        if (KT == 64) return launch_walk_tile<Ty, 64, 4, 1, NPX, MODE>(a, roles, n, st);
+        return launch_walk_tile<Ty, 128, 4, 1, NPX, MODE>(a, roles, n, st);
     }
-    if (KT == 32) return launch_walk_tile<Ty, 32, 8, NPX, MODE>(a, roles, n, st);
-    if (KT == 64) return launch_walk_tile<Ty, 64, 8, NPX, MODE>(a, roles, n, st);
-    return launch_walk_tile<Ty, 128, 8, NPX, MODE>(a, roles, n, st);
+    if (KT == 32) return launch_walk_tile<Ty, 32, 4, 2, NPX, MODE>(a, roles, n, st);
+    if (KT == 64) return launch_walk_tile<Ty, 64, 4, 2, NPX, MODE>(a, roles, n, st);
+    if constexpr (NPI == 3) return launch_walk_tile<Ty, 128, 8, 1, NPX, MODE>(a, roles, n, st);
+    else return launch_walk_tile<Ty, 128, 4, 2, NPX, MODE>(a, roles, n, st);
 }
 
 }  // namespace deer
