@@ -16,6 +16,7 @@ the current stream of the tensors' GPU.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import threading
 
@@ -450,9 +451,23 @@ def _operand(name, t, ref=None, shape=None, dtype=None):
         raise ValueError(f"{name} is on {t.device}, not on {ref.device}")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
     return t
+
+
+# the current stream of a GPU as an integer; torch's own call builds a Stream object first
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
+def _on(t):
+    """Makes t's GPU the current one (nothing to do if it is)."""
+    return contextlib.nullcontext() if torch.cuda.current_device() == t.device.index else torch.cuda.device(t.device)
 
 
 def _result(name, t, ref, shape, dtype):
@@ -532,7 +547,7 @@ def deer_linattn(q, k, v, log_decay, *, scale: float = 1.0, lengths=None, state0
     a = _Lin(q, k, v, log_decay, scale, lengths)
     if v.dim() != 4:
         raise ValueError("v must be [B, T, H, Dv]")
-    with torch.cuda.device(v.device):
+    with _on(v):
         o = _result("o", o, v, a.v.shape, v.dtype)
         s0 = a.matrix("state0", state0)
         if state is not None or want_state:
@@ -540,8 +555,8 @@ def deer_linattn(q, k, v, log_decay, *, scale: float = 1.0, lengths=None, state0
         if ws is None:
             ws = a.workspace(lib, _b.DEER_OP_SOLVE)
         st = lib.deer_linattn(ctypes.byref(a.c), a.B, a.T, ctypes.byref(a.vq), ctypes.byref(a.vk), ctypes.byref(a.vv),
-                              _ptr(a.log_decay), _ptr(a.lengths), _ptr(s0), _ptr(o), _ptr(state), _ptr(ws), ws.numel(),
-                              _stream())
+                              _at(a.log_decay), _at(a.lengths), _at(s0), _at(o), _at(state), _at(ws), ws.numel(),
+                              _raw_stream(v.device.index))
     _b._check(st, "deer_linattn")
     return {"o": o, "state": state}
 
@@ -555,7 +570,7 @@ def deer_linattn_adjoint(q, k, v, log_decay, g, *, scale: float = 1.0, lengths=N
     a = _Lin(q, k, v, log_decay, scale, lengths)
     if v.dim() != 4:
         raise ValueError("v must be [B, T, H, Dv]")
-    with torch.cuda.device(v.device):
+    with _on(v):
         gt, vg = _view(_operand("g", g, v, v.shape, v.dtype))
         s0, gs = a.matrix("state0", state0), a.matrix("g_state", g_state)
         grads = {"q": torch.empty(q.shape, dtype=q.dtype, device=v.device),
@@ -568,10 +583,10 @@ def deer_linattn_adjoint(q, k, v, log_decay, g, *, scale: float = 1.0, lengths=N
         if ws is None:
             ws = a.workspace(lib, _b.DEER_OP_ADJOINT)
         st = lib.deer_linattn_adjoint(ctypes.byref(a.c), a.B, a.T, ctypes.byref(a.vq), ctypes.byref(a.vk),
-                                      ctypes.byref(a.vv), _ptr(a.log_decay), _ptr(a.lengths), _ptr(s0),
-                                      ctypes.byref(vg), _ptr(gs), _ptr(grads["q"]), _ptr(grads["k"]), _ptr(grads["v"]),
-                                      _ptr(grads.get("log_decay")), _ptr(grads.get("state0")), _ptr(ws), ws.numel(),
-                                      _stream())
+                                      ctypes.byref(a.vv), _at(a.log_decay), _at(a.lengths), _at(s0),
+                                      ctypes.byref(vg), _at(gs), _at(grads["q"]), _at(grads["k"]), _at(grads["v"]),
+                                      _at(grads.get("log_decay")), _at(grads.get("state0")), _at(ws), ws.numel(),
+                                      _raw_stream(v.device.index))
     _b._check(st, "deer_linattn_adjoint")
     return {"grads": grads}
 
@@ -584,11 +599,11 @@ def deer_linattn_step(q, k, v, log_decay, state, *, scale: float = 1.0, lengths=
     a = _Lin(q, k, v, log_decay, scale, lengths)
     if v.dim() != 3:
         raise ValueError("v must be [B, H, Dv]")
-    with torch.cuda.device(v.device):
+    with _on(v):
         state = _result("state", _operand("state", state), v, (a.B, a.H, a.Dk, a.Dv), torch.float32)
         o = _result("o", o, v, a.v.shape, v.dtype)
         st = lib.deer_linattn_step(ctypes.byref(a.c), a.B, ctypes.byref(a.vq), ctypes.byref(a.vk), ctypes.byref(a.vv),
-                                   _ptr(a.log_decay), _ptr(a.lengths), _ptr(state), _ptr(o), _stream())
+                                   _at(a.log_decay), _at(a.lengths), _at(state), _at(o), _raw_stream(v.device.index))
     _b._check(st, "deer_linattn_step")
     return {"o": o, "state": state}
 
@@ -616,7 +631,7 @@ def _norm(x, w, b, eps):
     w, b = (None if t is None else t.contiguous() for t in (w, b))
     D = x.shape[-1]
     rows = x.numel() // D if D else 0
-    return x, w, b, rows, _b.deer_norm(_DTYPES[x.dtype], wtype, G, D, _ptr(w), _ptr(b), float(eps))
+    return x, w, b, rows, _b.deer_norm(_DTYPES[x.dtype], wtype, G, D, _at(w), _at(b), float(eps))
 
 
 def deer_layernorm_workspace_bytes(rows: int, G: int, D: int, dtype=torch.float32) -> int:
@@ -631,11 +646,11 @@ def deer_layernorm(x, w=None, b=None, *, eps: float = 1e-5, y=None) -> dict:
     head), float32 or x's type, or None.  Returns dict(y, mean, rstd), the statistics in float32."""
     lib = load()
     xc, wc, bc, rows, c = _norm(x, w, b, eps)
-    with torch.cuda.device(x.device):
+    with _on(x):
         y = _result("y", y, x, x.shape, x.dtype)
         mean = torch.empty(x.shape[:-1], device=x.device)
         rstd = torch.empty(x.shape[:-1], device=x.device)
-        st = lib.deer_layernorm(ctypes.byref(c), rows, _ptr(xc), _ptr(y), _ptr(mean), _ptr(rstd), _stream())
+        st = lib.deer_layernorm(ctypes.byref(c), rows, _at(xc), _at(y), _at(mean), _at(rstd), _raw_stream(x.device.index))
     _b._check(st, "deer_layernorm")
     return {"y": y, "mean": mean, "rstd": rstd}
 
@@ -645,7 +660,7 @@ def deer_layernorm_adjoint(x, g, mean, rstd, w=None, *, want_grads: bool = True,
     dL/dx in x's type, grads = {w, b} in float32, of w's shape ([D] without w); {} without want_grads)."""
     lib = load()
     xc, wc, _, rows, c = _norm(x, w, None, 0.0)
-    with torch.cuda.device(x.device):
+    with _on(x):
         gc = _operand("g", g, x, x.shape, x.dtype).contiguous()
         mc = _operand("mean", mean, x, x.shape[:-1], torch.float32).contiguous()
         rc = _operand("rstd", rstd, x, x.shape[:-1], torch.float32).contiguous()
@@ -657,7 +672,7 @@ def deer_layernorm_adjoint(x, g, mean, rstd, w=None, *, want_grads: bool = True,
         if ws is None:
             n = lib.deer_layernorm_workspace_bytes(ctypes.byref(c), rows)
             ws = torch.empty(max(int(n), 256), dtype=torch.uint8, device=x.device)
-        st = lib.deer_layernorm_adjoint(ctypes.byref(c), rows, _ptr(xc), _ptr(gc), _ptr(mc), _ptr(rc), _ptr(dx),
-                                        _ptr(grads.get("w")), _ptr(grads.get("b")), _ptr(ws), ws.numel(), _stream())
+        st = lib.deer_layernorm_adjoint(ctypes.byref(c), rows, _at(xc), _at(gc), _at(mc), _at(rc), _at(dx),
+                                        _at(grads.get("w")), _at(grads.get("b")), _at(ws), ws.numel(), _raw_stream(x.device.index))
     _b._check(st, "deer_layernorm_adjoint")
     return {"x": dx, "grads": grads}

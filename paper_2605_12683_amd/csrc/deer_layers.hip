@@ -55,19 +55,20 @@ static int seg_override() {
     return e ? atoi(e) : 0;
 }
 
-// Segments: enough that a walk's blocks fill the chip twice (two share a CU), none of fewer than
-// kMinSeg steps; one where the heads alone give half of that, since segments read k and v a second
-// time.  (2 x 4096 steps, 16 heads of 128 x 128 in bf16, where one segment gives 32 blocks: segments
-// of 256, 512, 1024, 4096 steps take 81, 79, 125, 304 us.)
-constexpr int kFillBlocks = 512, kMinSeg = 256;
+// Segments: enough that a walk's blocks fill the chip (two blocks share a CU, three of 64 columns),
+// none of fewer than kMinSeg steps; one where the heads alone give half of that, since segments read
+// k and v a second time.  (2 x 4096 steps, 16 heads of 128 x 128 in bf16, where one segment gives 32
+// blocks: segments of 256, 512, 1024, 4096 steps take 81, 79, 125, 304 us.)
+constexpr int kMinSeg = 256;
 
 static int segment_steps(const deer_linattn_shape *s, int B, int T, int op) {
     if (const int n = seg_override(); n > 0) return n >= T ? T : (n + 63) / 64 * 64;
     // the adjoint's walks of dq and dk run together, that of dv by itself
-    long blocks = (long)B * s->H * lin_tiles(s->Dk, s->Dv);
-    if (op == DEER_OP_ADJOINT) blocks = 2L * B * s->H * lin_tiles(s->Dv, s->Dk);
-    if (2 * blocks >= kFillBlocks || T <= kMinSeg) return T;
-    const long n = (kFillBlocks + blocks - 1) / blocks;
+    const bool adj = op == DEER_OP_ADJOINT;
+    const long blocks = (long)B * s->H * (adj ? 2 * lin_tiles(s->Dv, s->Dk) : lin_tiles(s->Dk, s->Dv));
+    const long fill = (adj ? s->Dk : s->Dv) <= 64 ? 768 : 512;
+    if (2 * blocks >= fill || T <= kMinSeg) return T;
+    const long n = (fill + blocks - 1) / blocks;
     const long steps = ((T + n - 1) / n + 63) / 64 * 64;
     return (int)(steps < kMinSeg ? kMinSeg : steps);
 }

@@ -30,6 +30,8 @@
 // below 80 KiB of LDS, C = 32 instead of 64 where needed, so that two blocks share a CU.
 #pragma once
 
+#include <type_traits>
+
 #include "launch.h"
 #include "split16.h"
 #include "types16.h"
@@ -95,7 +97,7 @@ struct LinTile {
     static constexpr int C = bytes(64) <= 80 * 1024 ? 64 : 32;
     static constexpr int lds = bytes(C);
     static constexpr int fit = 160 * 1024 / lds * NW / 4;
-    static constexpr int most = OUT && (CT == 2 || KT == 256) ? 2 : CT == 2 || KT == 256 ? 3 : 4;   // (registers)
+    static constexpr int most = KT == 256 || (CT == 2 && (OUT || KT == 128)) ? 2 : CT == 2 ? 3 : 4;   // (registers)
     static constexpr int waves = fit > most ? most : fit;           // per SIMD
 };
 
@@ -277,9 +279,14 @@ struct Decays {
     float hi[C], lo[C];   // log2 decay summed up to each step
     float into[C];        // sc_kv exp2(L - c): what a step's k v^T has left at the chunk's end
     float from[C];        // sc_o exp2(c): what the entering state has left at each step
-    float all;            // exp2(L)
-    float pad[3];
+    float all;            // factor on the registers that hold the state, at the chunk's end
+    float before, after;  // the state is this times the registers
+    float pad;
 };
+// The registers hold the state up to a factor 2^ls (the last wave's ls, shared through from, into,
+// before and after), so that the decay of a whole chunk costs no multiplication of every element:
+// it goes into ls, and the registers are only scaled where ls would leave +-kLazy.
+constexpr double kLazy = 24.0;
 
 // the double that the DPP control CTRL brings from another lane, 0 where it brings none
 template <int CTRL, int ROWS>
@@ -290,9 +297,10 @@ __device__ __forceinline__ double dpp_or_zero(double x) {
     return __builtin_bit_cast(double, ((uint64_t)h << 32) | l);
 }
 
-// by one wave; raw: this lane's log decay (C = 32: the upper half wave repeats the lower).  Returns L.
+// by one wave; raw: this lane's log decay (C = 32: the upper half wave repeats the lower), ls: of the
+// registers, before and after the chunk.  Returns L.
 template <int C>
-__device__ __forceinline__ double chunk_decays(Decays<C> &d, float raw, float sc_kv, float sc_o) {
+__device__ __forceinline__ double chunk_decays(Decays<C> &d, float raw, float sc_kv, float sc_o, double &ls) {
     const int lane = threadIdx.x & 63, i = lane & (C - 1);
     double s = gate_of(raw);
     s += dpp_or_zero<0x111, 15>(s);        // row_shr: lanes of each 16
@@ -308,9 +316,16 @@ __device__ __forceinline__ double chunk_decays(Decays<C> &d, float raw, float sc
     const float hi = (float)s;
     d.hi[i] = hi;
     d.lo[i] = (float)(s - (double)hi);
-    d.into[i] = sc_kv * __builtin_amdgcn_exp2f((float)(L - s));
-    d.from[i] = sc_o * __builtin_amdgcn_exp2f(hi);
-    if (i == 0) d.all = __builtin_amdgcn_exp2f((float)L);
+    d.from[i] = sc_o * __builtin_amdgcn_exp2f((float)(s + ls));
+    const double next = ls + L;
+    const bool lazy = next < kLazy && next > -kLazy;
+    d.into[i] = sc_kv * __builtin_amdgcn_exp2f((float)(lazy ? -(s + ls) : L - s));
+    if (i == 0) {
+        d.before = __builtin_amdgcn_exp2f((float)ls);
+        d.all = lazy ? 1.f : __builtin_amdgcn_exp2f((float)next);
+        d.after = lazy ? __builtin_amdgcn_exp2f((float)next) : 1.f;
+    }
+    ls = lazy ? next : 0.0;
     return L;
 }
 
@@ -376,6 +391,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
         return gate_raw(a, b, h, t0_of(n) + (rev ? C - 1 - i : i), len, rev);
     };
 
+    load(0);
     // Column c of the wave's tile ct is column n0 + col(c, ct): with two tiles a lane's four outputs
     // of both are eight columns in a row.
     auto col = [](int c, int ct) { return CT == 2 ? 8 * (c >> 2) + 4 * ct + (c & 3) : c; };
@@ -438,16 +454,16 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
         vr.template store<false>(Vs, PV);
         if constexpr (OUT) qr.template store<true>(Qs, PQ);
     };
-    load(0);
-    double total = 0.0;                                        // last wave: log2 decay of the segment
+    double total = 0.0, ls = 0.0;                              // last wave: log2 decay of the segment, the registers' scale
     float raw = 0.f;
     if (w == NW - 1) {
-        const double L = chunk_decays<C>(dec[0], gate(0), ro.sc_kv, ro.sc_o);
+        const double L = chunk_decays<C>(dec[0], gate(0), ro.sc_kv, ro.sc_o, ls);
         if (!OUT) total += L;
         raw = __int_as_float(afresh(__float_as_int(gate(1))));
     }
     const int na = (a.T + kLinAnchor - 1) / kLinAnchor;
     const float sc_p = ro.sc_kv * ro.sc_o;
+    const bool keep = ro.fin && a.nseg == 1;                   // the state behind the last step is wanted
     store();
 
     // The next chunk's rows are loaded while this one is computed and go to LDS before this one's
@@ -461,14 +477,14 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
             if (w == NW - 1) raw = gate(n + 2);
             load(n + 1);
             if (w == NW - 1) {
-                const double L = chunk_decays<C>(dec[(n + 1) & 1], next, ro.sc_kv, ro.sc_o);
+                const double L = chunk_decays<C>(dec[(n + 1) & 1], next, ro.sc_kv, ro.sc_o, ls);
                 if (!OUT) total += L;
             }
         }
         float *anc = nullptr;
         if constexpr (DOTS) {
             if ((t0 + C) % kLinAnchor == 0 || t0 + C >= a.T) anc = ro.anchor + ((size_t)bh * na + t0 / kLinAnchor) * mat;
-            if (anc && rev) put_state(anc, N, 1, 1.f);
+            if (anc && rev) put_state(anc, N, 1, dc.before);
         }
         __builtin_amdgcn_sched_barrier(0);
 
@@ -593,12 +609,17 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
             }
         };
 
-        // the chunk's own steps, and the state at its end
-        const float all = dc.all;
+        // the chunk's own steps, and (STATE) the state at its end
+        auto finish = [&](auto state) {
+        constexpr bool STATE = decltype(state)::value;
+        if constexpr (STATE) {
+            const float all = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(dc.all)));
+            if (all != 1.f)
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
+                for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct) S[dt][ct] *= all;
+                    for (int ct = 0; ct < CT; ++ct) S[dt][ct] *= all;
+        }
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             const int lane = lane_now(), g = lane >> 4, c = lane & 15;
@@ -636,6 +657,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
             if constexpr (OUT) read_p(0);
             else read_k(0);
             __builtin_amdgcn_sched_barrier(0);
+            if constexpr (STATE)
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
                 float x[8];
@@ -657,7 +679,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
                 for (int n = 0; n < PN; ++n) {
                     if (2 * ks + n * PB >= NT) break;
                     if (2 * ks + (n + 1) * PB < NT) read_p(n + 1);
-                    else read_k(0);
+                    else if (STATE) read_k(0);
                     __builtin_amdgcn_sched_barrier(0);
                     mfma_block<NPX - 1, CT, PB>(vf, pf[n & 1], [&](int ct, int m) -> v4f & { return O[2 * ks + n * PB + m][ct]; });
                     __builtin_amdgcn_sched_barrier(0);
@@ -665,6 +687,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
             }
             if constexpr (DOTS)
                 if (ks == KS - 1) read_partner();
+            if constexpr (STATE)
 #pragma unroll
             for (int n = 0; n < DT / KB; ++n) {
                 if (n + 1 < DT / KB) read_k(n + 1);
@@ -673,6 +696,9 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
+        };
+        if (!OUT || DOTS || n + 1 < chunks || keep) finish(std::true_type{});
+        else if constexpr (MODE == kOut) finish(std::false_type{});
 
         if constexpr (DOTS) {
             const int lane = lane_now(), g = lane >> 4, c = lane & 15;
@@ -694,7 +720,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
                 dot = group_sum(dot);
                 if (g == 0) dots[w * C + i] = t0 + (rev ? C - 1 - i : i) < len ? dot : 0.f;
             }
-            if (anc && !rev) put_state(anc, N, 1, 1.f);
+            if (anc && !rev) put_state(anc, N, 1, dc.after);
         }
         lds_barrier();
         if (n + 1 < chunks) {
@@ -763,10 +789,10 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
     if constexpr (OUT) {
         if (ro.fin && a.nseg == 1) {
             const float f = rev ? __builtin_amdgcn_exp2f((float)gate_of(gate_raw(a, b, h, -1, len, true))) : 1.f;
-            put_state(ro.fin + bh * mat, ro.fin_d, ro.fin_n, f);
+            put_state(ro.fin + bh * mat, ro.fin_d, ro.fin_n, f * dec[(chunks - 1) & 1].after);
         }
     } else {
-        put_state(ro.seg + ((size_t)bh * a.nseg + seg) * mat, N, 1, 1.f);
+        put_state(ro.seg + ((size_t)bh * a.nseg + seg) * mat, N, 1, dec[(chunks - 1) & 1].after);
         if (w == NW - 1 && (threadIdx.x & 63) == 0 && tile == 0)
             ro.seg_decay[(size_t)bh * a.nseg + seg] = __builtin_amdgcn_exp2f((float)total);
     }
