@@ -59,7 +59,7 @@ static int seg_override() {
 // none of fewer than kMinSeg steps; one where the heads alone give half of that, since segments read
 // k and v a second time.  (2 x 4096 steps, 16 heads of 128 x 128 in bf16, where one segment gives 32
 // blocks: segments of 256, 512, 1024, 4096 steps take 81, 79, 125, 304 us.)
-constexpr int kMinSeg = 256;
+constexpr int kMinSeg = 128;
 
 static int segment_steps(const deer_linattn_shape *s, int B, int T, int op) {
     if (const int n = seg_override(); n > 0) return n >= T ? T : (n + 63) / 64 * 64;

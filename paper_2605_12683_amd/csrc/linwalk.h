@@ -74,8 +74,8 @@ template <>
 struct InParts<F32> { static constexpr int n = 3; };
 
 // padded width of the summed side, and columns of the state per block: 128 where they fill more than
-// half of them and Kd <= 128, else 64.  A block has four waves of 32 or 16 columns; eight of 16 for
-// float32 tiles of 128 x 128, whose LDS leaves room for one block only.
+// half of them and Kd <= 128, else 64.  A block has four waves of 32 or 16 columns; with float32, whose
+// LDS tiles leave room for one or two blocks only, eight of 16 instead of four of 32.
 constexpr int kt_of(int Kd) { return Kd <= 32 ? 32 : Kd <= 64 ? 64 : Kd <= 128 ? 128 : 256; }
 constexpr int nb_of(int KT, int N) { return N > 64 && KT <= 128 ? 128 : 64; }
 
@@ -180,6 +180,10 @@ struct RowTile {
         for (int i = 0; i < NU; ++i) {
             const int n = i * TH + tid, row = n / UPR, d = (n % UPR) * E;
             if (C * UPR % TH != 0 && row >= C) continue;
+            if constexpr (NP == 1 && !PERM) {
+                *(v4u *)(lds + row * pitch + d) = u[i];
+                continue;
+            }
 #pragma unroll
             for (int half = 0; half < E / 4; ++half) {   // four elements at a time
                 uint32_t p[NP][2];
@@ -342,7 +346,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
     constexpr int NT = C / 16, KS = C / 32, DT = KT / 16;
     // operands read from LDS at a time: as many as the registers hold twice (dividing KT / 32, NT, DT)
     constexpr bool TIGHT = KT == 128 && Tile::waves == 4;
-    constexpr int UB = TIGHT && DOTS ? 1 : KT / 32 * NPI <= 4 ? KT / 32 : NPI == 1 ? 4 : NPI == 2 ? 2 : 1;
+    constexpr int UB = TIGHT || NPI == 3 || KT == 32 ? 1 : 2;
     constexpr int QB = TIGHT || CT == 2 || KT == 256 ? 2 : NT, KB = NPI == 1 && !TIGHT && DT > 2 ? 4 : 2, PB = NPX == 2 && !TIGHT ? 2 : 1;
     extern __shared__ __align__(16) unsigned char smem[];
     uint16_t *Ks = (uint16_t *)smem, *Vs = Ks + NPI * C * PK, *Qs = Vs + NPI * C * PV;
@@ -379,19 +383,16 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
     kr.init(ro.k, b, h, 0, Kd, rev, t0_of(0));
     vr.init(ro.v, b, h, col0, N, rev, t0_of(0));
     if constexpr (OUT) qr.init(ro.q, b, h, 0, Kd, rev, t0_of(0));
-    auto load = [&](int n) {                                   // of one chunk after the other
-        const int left = len - t0_of(n), rows = left < C ? left : C;
-        kr.load(rows);
-        vr.load(rows);
-        if constexpr (OUT) qr.load(rows);
-    };
+    auto rows_of = [&](int n) { return len - t0_of(n) < C ? len - t0_of(n) : C; };
     auto gate = [&](int n) {
         if (n >= chunks) return 0.f;
         const int i = threadIdx.x & (C - 1);
         return gate_raw(a, b, h, t0_of(n) + (rev ? C - 1 - i : i), len, rev);
     };
 
-    load(0);
+    kr.load(rows_of(0));
+    vr.load(rows_of(0));
+    if constexpr (OUT) qr.load(rows_of(0));
     // Column c of the wave's tile ct is column n0 + col(c, ct): with two tiles a lane's four outputs
     // of both are eight columns in a row.
     auto col = [](int c, int ct) { return CT == 2 ? 8 * (c >> 2) + 4 * ct + (c & 3) : c; };
@@ -472,10 +473,13 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
         const int t0 = t0_of(n);
         const Decays<C> &dc = dec[n & 1];
         lds_barrier();
-        if (n + 1 < chunks) {
+        const bool ahead = n + 1 < chunks;
+        const int rows_ahead = rows_of(n + 1);
+        if (ahead) {                    // (v's and q's rows follow between the products)
             const float next = raw;
             if (w == NW - 1) raw = gate(n + 2);
-            load(n + 1);
+            kr.load(rows_ahead);
+            if (!OUT) vr.load(rows_ahead);
             if (w == NW - 1) {
                 const double L = chunk_decays<C>(dec[(n + 1) & 1], next, ro.sc_kv, ro.sc_o, ls);
                 if (!OUT) total += L;
@@ -490,44 +494,69 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
 
         v4f O[NT][CT];
         if constexpr (OUT) {
-            // decayed scores, transposed: rows j, columns i
-            for (int tl = w; tl < NT * (NT + 1) / 2; tl += NW) {
+            // decayed scores, transposed (rows j, columns i): tiles w, w + NW, ... of those on and below
+            // the diagonal, a wave's tiles side by side so that their latencies overlap
+            constexpr int TRI = NT * (NT + 1) / 2, MOST = (TRI + NW - 1) / NW;
+            auto scores = [&](auto count) {
+                constexpr int M = decltype(count)::value;
                 const int lane = lane_now(), g = lane >> 4, c = lane & 15;
-                const int it = tl >= 6 ? 3 : tl >= 3 ? 2 : tl >= 1 ? 1 : 0, jt = tl - it * (it + 1) / 2;
-                const int i = it * 16 + c, j0 = jt * 16 + 4 * g;
-                const float hi_i = dc.hi[i], lo_i = dc.lo[i];
-                const v4f hi_j = *(const v4f *)(dc.hi + j0), lo_j = *(const v4f *)(dc.lo + j0);
-                v4f acc = {0.f, 0.f, 0.f, 0.f};
+                int it[M], jt[M];
+                float hi_i[M], lo_i[M];
+                v4f hi_j[M], lo_j[M], acc[M];
+#pragma unroll
+                for (int m = 0; m < M; ++m) {
+                    const int tl = w + m * NW;
+                    it[m] = tl >= 6 ? 3 : tl >= 3 ? 2 : tl >= 1 ? 1 : 0, jt[m] = tl - it[m] * (it[m] + 1) / 2;
+                    acc[m] = v4f{0.f, 0.f, 0.f, 0.f};
+                }
 #pragma unroll
                 for (int u0 = 0; u0 < KT / 32; u0 += UB) {
-                    v4u kf[UB][NPI], qf[UB][NPI];
+                    v4u kf[M][UB][NPI], qf[M][UB][NPI];
 #pragma unroll
-                    for (int u = 0; u < UB; ++u)
+                    for (int m = 0; m < M; ++m)
 #pragma unroll
-                        for (int p = 0; p < NPI; ++p) {
-                            const uint16_t *kp = Ks + (p * C + jt * 16 + c) * PK + (u0 + u) * 32 + 4 * g;
-                            const v2u k0 = *(const v2u *)kp, k1 = *(const v2u *)(kp + 16);
-                            kf[u][p] = v4u{k0[0], k0[1], k1[0], k1[1]};
-                            qf[u][p] = *(const v4u *)(Qs + (p * C + it * 16 + c) * PQ + (u0 + u) * 32 + 8 * g);
+                        for (int u = 0; u < UB; ++u)
+#pragma unroll
+                            for (int p = 0; p < NPI; ++p) {
+                                const uint16_t *kp = Ks + (p * C + jt[m] * 16 + c) * PK + (u0 + u) * 32 + 4 * g;
+                                const v2u k0 = *(const v2u *)kp, k1 = *(const v2u *)(kp + 16);
+                                kf[m][u][p] = v4u{k0[0], k0[1], k1[0], k1[1]};
+                                qf[m][u][p] = *(const v4u *)(Qs + (p * C + it[m] * 16 + c) * PQ + (u0 + u) * 32 + 8 * g);
+                            }
+                    if (u0 + UB >= KT / 32)
+#pragma unroll
+                        for (int m = 0; m < M; ++m) {
+                            hi_i[m] = dc.hi[it[m] * 16 + c], lo_i[m] = dc.lo[it[m] * 16 + c];
+                            hi_j[m] = *(const v4f *)(dc.hi + jt[m] * 16 + 4 * g);
+                            lo_j[m] = *(const v4f *)(dc.lo + jt[m] * 16 + 4 * g);
                         }
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int u = 0; u < UB; ++u) acc = mfma_parts<NPI - 1>(kf[u], qf[u], acc);
-                }
-                float x[4];
+                    for (int u = 0; u < UB; ++u)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float e = (hi_i - hi_j[r]) + (lo_i - lo_j[r]);
-                    const float p = acc[r] * sc_p * __builtin_amdgcn_exp2f(e);
-                    x[r] = j0 + r <= i ? p : 0.f;
+                        for (int m = 0; m < M; ++m) acc[m] = mfma_parts<NPI - 1>(kf[m][u], qf[m][u], acc[m]);
                 }
-                uint32_t *dst = (uint32_t *)(Ps + pair(it, jt >> 1) * NPX * 64 + lane) + (jt & 1) * 2;
-                uint32_t p0[3], p1[3];
-                split_pair(x[0], x[1], p0);
-                split_pair(x[2], x[3], p1);
 #pragma unroll
-                for (int q = 0; q < NPX; ++q) *(v2u *)(dst + q * 64 * 4) = v2u{p0[q], p1[q]};
-            }
+                for (int m = 0; m < M; ++m) {
+                    const int above = it[m] == jt[m] ? 4 * g - c : -64;   // j - i of the first row, on the diagonal
+                    float x[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float e = (hi_i[m] - hi_j[m][r]) + (lo_i[m] - lo_j[m][r]);
+                        const float p = acc[m][r] * sc_p * __builtin_amdgcn_exp2f(e);
+                        x[r] = above + r <= 0 ? p : 0.f;
+                    }
+                    uint32_t *dst = (uint32_t *)(Ps + pair(it[m], jt[m] >> 1) * NPX * 64 + lane) + (jt[m] & 1) * 2;
+                    uint32_t p0[3], p1[3];
+                    split_pair(x[0], x[1], p0);
+                    split_pair(x[2], x[3], p1);
+#pragma unroll
+                    for (int q = 0; q < NPX; ++q) *(v2u *)(dst + q * 64 * 4) = v2u{p0[q], p1[q]};
+                }
+            };
+            if (w + (MOST - 1) * NW < TRI) scores(std::integral_constant<int, MOST>{});
+            else if constexpr (MOST > 1) scores(std::integral_constant<int, MOST - 1>{});
+            if (ahead) vr.load(rows_ahead);
             // what the entering state gives, transposed: rows n, columns i
             const int lane = lane_now(), g = lane >> 4, c = lane & 15;
 #pragma unroll
@@ -568,6 +597,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) O[it][ct] *= f;
             }
+            if (ahead) qr.load(rows_ahead);
             lds_barrier();
         }
 
@@ -697,7 +727,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
             }
         }
         };
-        if (!OUT || DOTS || n + 1 < chunks || keep) finish(std::true_type{});
+        if (!OUT || DOTS || ahead || keep) finish(std::true_type{});
         else if constexpr (MODE == kOut) finish(std::false_type{});
 
         if constexpr (DOTS) {
@@ -723,7 +753,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
             if (anc && !rev) put_state(anc, N, 1, dc.after);
         }
         lds_barrier();
-        if (n + 1 < chunks) {
+        if (ahead) {
             store();
             raw = __int_as_float(afresh(__float_as_int(raw)));   // (loaded before the rows: no wait for it later)
         }
@@ -829,10 +859,10 @@ int launch_walk_parts(const LinArgs &a, const LinRole *roles, int n, hipStream_t
         if (KT == 64) return launch_walk_tile<Ty, 64, 4, 1, NPX, MODE>(a, roles, n, st);
         return launch_walk_tile<Ty, 128, 4, 1, NPX, MODE>(a, roles, n, st);
     }
-    if (KT == 32) return launch_walk_tile<Ty, 32, 4, 2, NPX, MODE>(a, roles, n, st);
-    if (KT == 64) return launch_walk_tile<Ty, 64, 4, 2, NPX, MODE>(a, roles, n, st);
-    if constexpr (NPI == 3) return launch_walk_tile<Ty, 128, 8, 1, NPX, MODE>(a, roles, n, st);
-    else return launch_walk_tile<Ty, 128, 4, 2, NPX, MODE>(a, roles, n, st);
+    constexpr int NW = NPI == 3 ? 8 : 4, CT = 8 / NW;
+    if (KT == 32) return launch_walk_tile<Ty, 32, NW, CT, NPX, MODE>(a, roles, n, st);
+    if (KT == 64) return launch_walk_tile<Ty, 64, NW, CT, NPX, MODE>(a, roles, n, st);
+    return launch_walk_tile<Ty, 128, NW, CT, NPX, MODE>(a, roles, n, st);
 }
 
 }  // namespace deer
