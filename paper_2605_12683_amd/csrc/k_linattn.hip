@@ -247,42 +247,75 @@ __device__ __forceinline__ const typename Ty::T *row_of(const LinView &x, int b,
     return (const typename Ty::T *)x.p + b * x.sb + (h / x.r) * x.sh;
 }
 
-// One block per 64 columns of one head's state; a thread owns one column of every 4th row.
-template <class Ty>
+// One block per 64 columns of one head's state, which is read and written once: memory bounds a batch
+// (256 sequences, 32 heads of 128 x 128: 1.08 GB), latency a single sequence.  A thread owns W
+// columns of every (4 W)th row, up to eight rows loaded before the first is used; W = 4 where Dv and
+// the state's address allow loads of 16 bytes.
+template <class Ty, int W>
 __global__ __launch_bounds__(256) void k_lin_step(LinStep a) {
-    __shared__ float qs[256], ks[256], red[4][64];
+    constexpr int LC = 64 / W, RG = 256 / LC, U = 8;   // lanes per row, rows at a time, rows in flight
+    __shared__ float qs[256], ks[256], red[RG][64];
     const int tiles = (a.Dv + 63) / 64, tile = blockIdx.x % tiles, bh = blockIdx.x / tiles;
-    const int b = bh / a.H, h = bh % a.H, c = threadIdx.x & 63, w = threadIdx.x >> 6, n = tile * 64 + c;
+    const int b = bh / a.H, h = bh % a.H, cl = threadIdx.x % LC, rg = threadIdx.x / LC, n = tile * 64 + cl * W;
     const bool on = n < a.Dv;
-    typename Ty::T *o = (typename Ty::T *)a.o + (size_t)bh * a.Dv + n;
+    typename Ty::T *o = (typename Ty::T *)a.o + (size_t)bh * a.Dv + tile * 64;
     if (a.lengths && a.lengths[b] <= 0) {
-        if (w == 0 && on) *o = Ty::down(0.f);
+        if (threadIdx.x < 64 && tile * 64 + (int)threadIdx.x < a.Dv) o[threadIdx.x] = Ty::down(0.f);
         return;
     }
+    typedef float vf __attribute__((ext_vector_type(W)));
+    vf *S = (vf *)(a.state + (size_t)bh * a.Dk * a.Dv + n);
+    const size_t row = a.Dv / W;                       // in vf
+    vf s[U];
+    auto load = [&](int d0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (on && d0 + u * RG < a.Dk) s[u] = S[(size_t)(d0 + u * RG) * row];
+    };
+    load(rg);
     const typename Ty::T *q = row_of<Ty>(a.q, b, h), *k = row_of<Ty>(a.k, b, h);
     for (int d = threadIdx.x; d < a.Dk; d += 256) qs[d] = Ty::up(q[d]), ks[d] = Ty::up(k[d]);
-    __syncthreads();
     const float g = __builtin_amdgcn_exp2f((float)gate_of(a.log_decay[a.per_seq ? (size_t)bh : h]));
-    float acc = 0.f;
-    if (on) {
-        const float v = Ty::up(row_of<Ty>(a.v, b, h)[n]);
-        float *S = a.state + (size_t)bh * a.Dk * a.Dv + n;
-        for (int d = w; d < a.Dk; d += 4) {
-            const float s = fmaf(ks[d], v, g * S[(size_t)d * a.Dv]);
-            S[(size_t)d * a.Dv] = s;
-            acc = fmaf(qs[d], s, acc);
+    vf v = {}, acc = {};
+    if (on)
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] = Ty::up(row_of<Ty>(a.v, b, h)[n + i]);
+    lds_barrier();
+    for (int d0 = rg; d0 < a.Dk; d0 += U * RG) {
+        if (d0 != rg) load(d0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int d = d0 + u * RG;
+            if (!on || d >= a.Dk) continue;
+            const float kd = ks[d], qd = qs[d];
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                s[u][i] = fmaf(kd, v[i], g * s[u][i]);
+                acc[i] = fmaf(qd, s[u][i], acc[i]);
+            }
+            S[(size_t)d * row] = s[u];
         }
     }
-    red[w][c] = acc;
-    __syncthreads();
-    if (w == 0 && on) *o = Ty::down(a.scale * ((red[0][c] + red[1][c]) + (red[2][c] + red[3][c])));
+#pragma unroll
+    for (int i = 0; i < W; ++i) red[rg][cl * W + i] = acc[i];
+    lds_barrier();
+    if (threadIdx.x < 64 && tile * 64 + (int)threadIdx.x < a.Dv) {
+        float x = 0.f;
+#pragma unroll
+        for (int i = 0; i < RG; ++i) x += red[i][threadIdx.x];
+        o[threadIdx.x] = Ty::down(a.scale * x);
+    }
 }
 
 int launch_lin_step(const LinStep &a, hipStream_t st) {
     return with_dtype(a.dtype, [&](auto ty) {
         using Ty = decltype(ty);
         KTimer kt("k_lin_step", st);
-        hipLaunchKernelGGL(k_lin_step<Ty>, dim3(a.B * a.H * ((a.Dv + 63) / 64)), dim3(256), 0, st, a);
+        const dim3 grid(a.B * a.H * ((a.Dv + 63) / 64));
+        if (a.Dv % 4 == 0 && ((uintptr_t)a.state & 15) == 0)
+            hipLaunchKernelGGL((k_lin_step<Ty, 4>), grid, dim3(256), 0, st, a);
+        else
+            hipLaunchKernelGGL((k_lin_step<Ty, 1>), grid, dim3(256), 0, st, a);
         DEER_LAUNCH_CHECK("k_lin_step");
         return (int)DEER_OK;
     });
