@@ -57,7 +57,7 @@ __device__ __forceinline__ void load_weights(const NormArgs &a, const void *w, i
         }
 }
 
-constexpr int block_of(int team) { return team < 256 ? 256 : team; }
+constexpr int block_of(int team) { return team <= 64 ? 256 : team; }   // a team of several waves has its block to itself
 
 template <class Ty, int TEAM, int NV>
 __global__ __launch_bounds__(block_of(TEAM)) void k_layernorm(NormArgs a, int nt, bool vec, typename Ty::T *y,
@@ -310,8 +310,9 @@ __global__ __launch_bounds__(256) void k_layernorm_long_part(NormArgs a, const t
 
 // ---- launches -------------------------------------------------------------------------------------
 
-// threads per row and units per thread, at most 16 elements a thread (the adjoint holds six float32
-// values of each); 0: none does
+// threads per row and units per thread: two units where a row has them, so that enough is in flight
+// (rows of 2048 in bf16: 53 us with 128 threads, 62 us with 256 of one unit); at most 16 elements a
+// thread, of which the adjoint holds six float32 values each; 0: none holds the row
 struct NormShape {
     int team, nv;
 };
@@ -320,7 +321,7 @@ static NormShape shape_of(int dtype, int D) {
     if (u <= 16) return {16, 1};
     if (u <= 64) return {64, 1};
     if (u <= 128) return {64, 2};
-    if (u <= 256) return {256, 1};
+    if (u <= 256) return {128, 2};
     if (u <= 512) return {256, 2};
     if (u <= 1024) return {512, 2};
     if (u <= 2048) return {1024, 2};
@@ -352,7 +353,8 @@ static int with_shape(const NormArgs &a, Fn f) {
     return with_dtype(a.dtype, [&](auto ty) {
         if (s.team == 16) return f(ty, Int<16>{}, Int<1>{});
         if (s.team == 64) return s.nv == 1 ? f(ty, Int<64>{}, Int<1>{}) : f(ty, Int<64>{}, Int<2>{});
-        if (s.team == 256) return s.nv == 1 ? f(ty, Int<256>{}, Int<1>{}) : f(ty, Int<256>{}, Int<2>{});
+        if (s.team == 128) return f(ty, Int<128>{}, Int<2>{});
+        if (s.team == 256) return f(ty, Int<256>{}, Int<2>{});
         if (s.team == 512) return f(ty, Int<512>{}, Int<2>{});
         if constexpr (std::is_same<decltype(ty), F32>::value)
             if (s.nv == 4) return f(ty, Int<1024>{}, Int<4>{});
