@@ -354,14 +354,14 @@ typedef struct {
 } deer_view;
 
 /* Workspace bytes of deer_linattn (op = DEER_OP_SOLVE) and deer_linattn_adjoint
- * (DEER_OP_ADJOINT).  Returns 0 for invalid arguments. */
+ * (DEER_OP_ADJOINT).  Returns 0 for invalid arguments (sizes: T up to 2^30, B T H up to 2^33). */
 size_t deer_linattn_workspace_bytes(const deer_linattn_shape *shape, int B, int T, int op);
 
 /* The whole sequence.
  *   log_decay  float32 [H] or [B, T, H] (per_step).  Values are meant to be <= 0; -inf is a
  *              decay of zero: the state starts anew at that step (recordings laid end to end).
  *              Positive values grow the state and are exact as long as the products of the
- *              decays over any 64 steps and the states stay in float32's range.
+ *              decays over any 64 steps stay below 2^100 and the states in float32's range.
  *   lengths    int32 [B] or NULL (T): sequence b has lengths[b] steps (clamped to 0..T).  Rows
  *              at and behind its end are not read; their outputs are zero.
  *   state0     float32 [B, H, Dk, Dv] or NULL (zero): the state before the first step.

@@ -23,7 +23,10 @@ static int check_shape(const deer_linattn_shape *s, int B, int T) {
     }
     if (!isfinite(s->scale)) { set_error("scale must be finite"); return DEER_ERR_INVALID_ARG; }
     if ((long)B * s->H > (1L << 20)) { set_error("B H must not exceed 2^20 (B=%d, H=%d)", B, s->H); return DEER_ERR_INVALID_ARG; }
-    if ((long)B * T > (1L << 31)) { set_error("B*T too large"); return DEER_ERR_INVALID_ARG; }
+    if (T > (1 << 30) || (double)B * T * s->H > 8589934592.0) {
+        set_error("T must not exceed 2^30, nor B T H 2^33 (B=%d, T=%d, H=%d)", B, T, s->H);
+        return DEER_ERR_INVALID_ARG;
+    }
     return DEER_OK;
 }
 
@@ -44,8 +47,9 @@ static int check_alias(const void *out, const char *name, const void *const *in,
     return DEER_OK;
 }
 
+// (a single step's stride says nothing: one that leaves its rows aligned and apart)
 static LinView view_of(const deer_view *x, int r, int T) {
-    return {x->p, (long)x->sb, T > 1 ? (long)x->st : 0, (long)x->sh, r};
+    return {x->p, (long)x->sb, T > 1 ? (long)x->st : 256, (long)x->sh, r};
 }
 
 // DEER_LIN_SEG=n: segments of n steps (rounded up to 64), whatever the sizes (a tuning and test

@@ -117,7 +117,9 @@ __device__ __forceinline__ int afresh(int x) {
     return x;
 }
 
-// offsets of 2^31 or more lie outside every resource used here: loads give zero, stores are dropped
+// Offsets of 2^31 or more lie outside every resource used here: loads give zero, stores are dropped.
+// (A resource spans C rows of at most 2^24 bytes, 2^30; an offset outside that is moved by less than
+// 2^30 either way still lies beyond it.)
 constexpr uint32_t kOutside = 0x80000000u;
 
 // One operand's rows of one (sequence, head): W columns from col0 on, C rows a chunk, NU units of 16
@@ -130,7 +132,7 @@ struct RowTile {
     static constexpr int E = 16 / sizeof(T), UPR = W / E, NU = (C * UPR + TH - 1) / TH, ROWS = TH / UPR;
     const char *base;              // of the next chunk
     int st, col0, width, step;     // st, step in bytes
-    int off;                       // of the first unit
+    uint32_t off;                  // of the first unit
     bool fast, rev;
     v4u u[NU];
 
@@ -139,18 +141,18 @@ struct RowTile {
         st = (int)(x.st * (long)sizeof(T)), col0 = col0_, width = width_, rev = rev_;
         step = rev ? -ROWS * st : ROWS * st;
         const int row = threadIdx.x / UPR, d = col0 + threadIdx.x % UPR * E;
-        off = d < width && row < C ? (rev ? C - 1 - row : row) * st + d * (int)sizeof(T) : (int)kOutside;
+        off = d < width && row < C ? (uint32_t)((rev ? C - 1 - row : row) * st + d * (int)sizeof(T)) : kOutside;
         fast = (((uintptr_t)base | (uintptr_t)st) & 15) == 0 && width % E == 0 && x.st >= width;
     }
 
     __device__ __forceinline__ void load(int rows) {           // rows: how many exist, any number below 1 for none
         const auto rs = bounded_rsrc(base, rows > 0 ? (uint32_t)((rows - 1) * st + width * (int)sizeof(T)) : 0u);
         base += (long)(rev ? -C : C) * st;
-        const int o = afresh(off);
+        const uint32_t o = (uint32_t)afresh((int)off);
         if (fast) {
 #pragma unroll
             for (int i = 0; i < NU; ++i)
-                u[i] = __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(rs, o + i * step, 0, 0));
+                u[i] = __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)(o + (uint32_t)(i * step)), 0, 0));
             return;
         }
         const int tid = afresh((int)threadIdx.x), d = col0 + tid % UPR * E;
@@ -161,9 +163,9 @@ struct RowTile {
             uint32_t x[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const int at = on && d + e < width ? o + i * step + e * (int)sizeof(T) : (int)kOutside;
-                if constexpr (sizeof(T) == 4) x[e] = bload_u(rs, (uint32_t)at, 0);
-                else x[e] = __builtin_bit_cast(uint16_t, __builtin_amdgcn_raw_buffer_load_b16(rs, at, 0, 0));
+                const uint32_t at = on && d + e < width ? o + (uint32_t)(i * step + e * (int)sizeof(T)) : kOutside;
+                if constexpr (sizeof(T) == 4) x[e] = bload_u(rs, at, 0);
+                else x[e] = __builtin_bit_cast(uint16_t, __builtin_amdgcn_raw_buffer_load_b16(rs, (int)at, 0, 0));
             }
 #pragma unroll
             for (int k = 0; k < 4; ++k) u[i][k] = sizeof(T) == 4 ? x[k] : x[2 * k] | x[2 * k + 1] << 16;
@@ -436,7 +438,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
     const int out_size = ro.out_f32 ? 4 : (int)sizeof(T), out_row = a.H * N * out_size;   // C rows below 2^31 bytes
     auto out_off = [&](int l, int row, int size) {             // of it = 0; the others 16 rows further each
         const int n = n0 + 4 * CT * (l >> 4);
-        return n < N ? (rev ? C - 1 - (l & 15) : l & 15) * row + n * size : (int)kOutside;
+        return n < N ? (uint32_t)((rev ? C - 1 - (l & 15) : l & 15) * row + n * size) : kOutside;
     };
     const T *partner = nullptr;
     bool partner_fast = false;
@@ -608,18 +610,18 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
             const auto prs = bounded_rsrc(partner + t0 * ro.partner.st,
                                           rows > 0 ? (uint32_t)(((rows - 1) * ro.partner.st + N) * sizeof(T)) : 0u);
             const int row = (int)(ro.partner.st * (long)sizeof(T)), l = afresh((int)threadIdx.x) & 63;
-            const int off0 = out_off(l, row, sizeof(T));
+            const uint32_t off0 = out_off(l, row, sizeof(T));
 #pragma unroll
             for (int it = 0; it < NT; ++it) {
-                const int off = off0 + (rev ? -16 * it : 16 * it) * row;
+                const uint32_t off = off0 + (uint32_t)((rev ? -16 * it : 16 * it) * row);
                 if (partner_fast) {
                     if constexpr (4 * CT * sizeof(T) == 8) {
-                        const v2u x = __builtin_bit_cast(v2u, __builtin_amdgcn_raw_buffer_load_b64(prs, off, 0, 0));
+                        const v2u x = __builtin_bit_cast(v2u, __builtin_amdgcn_raw_buffer_load_b64(prs, (int)off, 0, 0));
                         pr[it][0] = v4u{x[0], x[1], 0, 0};
                     } else {
 #pragma unroll
                         for (int k = 0; k < PW; ++k)
-                            pr[it][k] = __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(prs, off + 16 * k, 0, 0));
+                            pr[it][k] = __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(prs, (int)(off + 16 * k), 0, 0));
                     }
                     continue;
                 }
@@ -628,11 +630,11 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
                 for (int k = 0; k < PW; ++k) pr[it][k] = v4u{0, 0, 0, 0};
 #pragma unroll
                 for (int e = 0; e < 4 * CT; ++e) {
-                    const int p = j < rows && nn + e < N ? off + e * (int)sizeof(T) : (int)kOutside;
+                    const uint32_t p = j < rows && nn + e < N ? off + e * (uint32_t)sizeof(T) : kOutside;
                     if constexpr (sizeof(T) == 4)
-                        pr[it][e / 4][e % 4] = bload_u(prs, (uint32_t)p, 0);
+                        pr[it][e / 4][e % 4] = bload_u(prs, p, 0);
                     else
-                        pr[it][e / 8][e / 2 % 4] |= (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(prs, p, 0, 0)
+                        pr[it][e / 8][e / 2 % 4] |= (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(prs, (int)p, 0, 0)
                                                     << (e & 1) * 16;
                 }
                 __builtin_amdgcn_sched_barrier(0);
@@ -771,22 +773,23 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
             const size_t first = (((size_t)b * a.T + t0) * a.H + h) * N;
             const auto ors = bounded_rsrc((char *)ro.out + first * out_size,
                                           (uint32_t)((rows - 1) * out_row + N * out_size));
-            const int off0 = out_off(l, out_row, out_size), step = (rev ? -16 : 16) * out_row;
+            const uint32_t off0 = out_off(l, out_row, out_size);
+            auto off_of = [&](int it) { return off0 + (uint32_t)((rev ? -16 * it : 16 * it) * out_row); };
             if (ro.wide_out && (sizeof(T) == 4 || ro.out_f32)) {
 #pragma unroll
                 for (int it = 0; it < NT; ++it)
 #pragma unroll
                     for (int ct = 0; ct < CT; ++ct)
                         __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, O[it][ct]), ors,
-                                                               off0 + it * step + ct * 16, 0, 0);
+                                                               (int)(off_of(it) + ct * 16), 0, 0);
             } else if (ro.wide_out) {
 #pragma unroll
                 for (int it = 0; it < NT; ++it) {
                     union { T x[4 * CT]; v2u u; v4u v; } y;
 #pragma unroll
                     for (int e = 0; e < 4 * CT; ++e) y.x[e] = Ty::down(O[it][e / 4][e % 4]);
-                    if constexpr (CT == 2) __builtin_amdgcn_raw_buffer_store_b128(y.v, ors, off0 + it * step, 0, 0);
-                    else __builtin_amdgcn_raw_buffer_store_b64(y.u, ors, off0 + it * step, 0, 0);
+                    if constexpr (CT == 2) __builtin_amdgcn_raw_buffer_store_b128(y.v, ors, (int)off_of(it), 0, 0);
+                    else __builtin_amdgcn_raw_buffer_store_b64(y.u, ors, (int)off_of(it), 0, 0);
                 }
             } else {
                 const int nn = n0 + 4 * CT * (l >> 4);
@@ -794,12 +797,12 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
                 for (int it = 0; it < NT; ++it)
 #pragma unroll
                     for (int e = 0; e < 4 * CT; ++e) {
-                        const int p = nn + e < N ? off0 + it * step + e * out_size : (int)kOutside;
+                        const uint32_t p = nn + e < N ? off_of(it) + e * out_size : kOutside;
                         const float o = O[it][e / 4][e % 4];
                         if (sizeof(T) == 4 || ro.out_f32) {
-                            bstore_u(ors, __float_as_uint(o), (uint32_t)p, 0);
+                            bstore_u(ors, __float_as_uint(o), p, 0);
                         } else if constexpr (sizeof(T) == 2) {
-                            __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, (T)Ty::down(o)), ors, p, 0, 0);
+                            __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, (T)Ty::down(o)), ors, (int)p, 0, 0);
                         }
                         if (e == 4 * CT - 1) __builtin_amdgcn_sched_barrier(0);
                     }

@@ -171,6 +171,35 @@ def test_decays_of_every_size(type_):
 
 
 @pytest.mark.parametrize("type_", ["f32", "bf16"])
+def test_growth(type_):
+    """States that grow for a while (by e^0.9 a step for 60 steps, 2^78) and decay again."""
+    c, kw, g, gs = make(1, 200, 2, 1, 16, 24, type_, True, True)
+    c["log_decay"][0, 30:90, 0] = 0.9
+    c["log_decay"][0, 90:150, 0] = -0.8
+    c["log_decay"][0, 60:70, 1] = 3.0
+    say("linattn growth", type_)
+    check_forward(c, kw)
+    check_adjoint(c, kw, g, gs)
+
+
+SEG_CASES = [(1, 1300, 2, 1, 24, 40, "bf16", [1300]), (2, 700, 2, 2, 130, 70, "f32", [700, 257]),
+             (3, 640, 1, 1, 64, 64, "f16", [640, 64, 0]), (1, 2500, 1, 1, 96, 256, "bf16", [2111]),
+             (2, 1100, 2, 1, 128, 128, "bf16", [1100, 1025]), (1, 200, 1, 1, 40, 31, "f32", [200])]
+
+
+@pytest.mark.parametrize("B,T,H,Hk,Dk,Dv,type_,lengths", SEG_CASES)
+@pytest.mark.parametrize("seg", [64, 128, 320, 1 << 20])
+@pytest.mark.parametrize("state", [False, True])
+def test_segments(B, T, H, Hk, Dk, Dv, type_, lengths, seg, state, monkeypatch):
+    """Segments of every length (and one only), with ends of sequences inside, between and before them."""
+    monkeypatch.setenv("DEER_LIN_SEG", str(seg))
+    c, kw, g, gs = make(B, T, H, Hk, Dk, Dv, type_, seg == 128, state, lengths)
+    say("linattn segments", B, T, H, Hk, Dk, Dv, type_, seg, state)
+    check_forward(c, kw)
+    check_adjoint(c, kw, g, gs)
+
+
+@pytest.mark.parametrize("type_", ["f32", "bf16"])
 def test_rows_behind_the_end_are_not_read(type_):
     """Lengths from below zero to beyond T; NaN and infinities behind the ends."""
     B, T = 6, 133
@@ -211,7 +240,10 @@ def test_views(type_, Dk, Dv):
     shared = [x[:1].expand(B, T, H, x.shape[-1]) for x in (q, k, v)]
     ld = -torch.rand(B, H, T, device="cuda", generator=gen).transpose(1, 2)
     g = torch.randn(B, H, T, Dv, device="cuda", generator=gen).to(t).transpose(1, 2)
-    for ops in ((q, k, v), swapped, dense_last, shared):
+    one_step = [x[:, :1].expand(B, T, H, x.shape[-1]) for x in (q, k, v)]
+    near_rows = [torch.randn(B, T * 2 + x.shape[-1] + 64, device="cuda", generator=gen).to(t).as_strided(
+        (B, T, H, x.shape[-1]), (T * 2 + x.shape[-1] + 64, 2, 16, 1)) for x in (q, k, v)]     # rows that overlap
+    for ops in ((q, k, v), swapped, dense_last, shared, one_step, near_rows):
         kw = {"scale": 0.2}
         a = D.deer_linattn(*ops, ld, want_state=True, **kw)
         b = D.deer_linattn(*(x.contiguous() for x in ops), ld.contiguous(), want_state=True, **kw)
@@ -219,6 +251,32 @@ def test_views(type_, Dk, Dv):
         a = D.deer_linattn_adjoint(*ops, ld, g, **kw)["grads"]
         b = D.deer_linattn_adjoint(*(x.contiguous() for x in ops), ld.contiguous(), g.contiguous(), **kw)["grads"]
         assert all(torch.equal(a[n], b[n]) for n in a)
+
+
+@pytest.mark.parametrize("type_,T", [("bf16", 400), ("f32", 200), ("bf16", 1)])
+def test_wide_step_strides(type_, T):
+    """Tensors with the largest stride of a step that is taken (2^22 elements); one above it is refused."""
+    t = TYPES[type_]
+    say("linattn wide strides", type_, T)
+    B, H, Dk, Dv = 1, 2, 32, 64
+    c, kw, g, _ = make(B, T, H, H, Dk, Dv, type_)
+    views = {}
+    far = torch.empty((T - 1) * (1 << 22) + 1000, dtype=t, device="cuda")
+    at = 0
+    for n in ("q", "k", "v"):
+        views[n] = far.as_strided(c[n].shape, (64, 1 << 22, c[n].shape[3], 1), at)
+        views[n].copy_(c[n])
+        at += H * c[n].shape[3]
+    ref = D.deer_linattn(**c, want_state=True, **kw)
+    a = D.deer_linattn(**views, log_decay=c["log_decay"], want_state=True, **kw)
+    assert torch.equal(a["o"], ref["o"]) and torch.equal(a["state"], ref["state"])
+    ga = D.deer_linattn_adjoint(**views, log_decay=c["log_decay"], g=g, **kw)["grads"]
+    gb = D.deer_linattn_adjoint(**c, g=g, **kw)["grads"]
+    assert all(torch.equal(ga[n], gb[n]) for n in ga)
+    if T > 1:
+        wider = {n: far.as_strided((1, 2, *c[n].shape[2:]), (64, (1 << 22) + 8, c[n].shape[3], 1)) for n in ("q", "k", "v")}
+        with pytest.raises(D.DeerError, match="stride"):
+            D.deer_linattn(**wider, log_decay=c["log_decay"], **kw)
 
 
 def test_offsets_beyond_32_bits():

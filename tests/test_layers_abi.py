@@ -30,7 +30,7 @@ def _view(p, sb=64, st=32, sh=8):
 
 
 BAD_SHAPES = [dict(dtype=3), dict(dtype=-1), dict(H=0), dict(Hk=0), dict(H=3), dict(H=1), dict(Dk=0), dict(Dk=257),
-              dict(Dv=0), dict(Dv=257), dict(scale=float("nan")), dict(scale=float("inf")), dict(H=1 << 21, Hk=1)]
+              dict(Dv=0), dict(Dv=257), dict(scale=float("nan")), dict(scale=float("inf")), dict(H=1 << 21, Hk=1), dict(H=16385, Hk=1)]
 
 
 @pytest.mark.parametrize("kw", BAD_SHAPES)
@@ -48,7 +48,7 @@ def test_shapes(lib, kw):
 
 def test_sizes_and_queries(lib):
     s = _shape()
-    for B, T in ((0, 4), (4, 0), (-1, 4), (1 << 19, 4), (1 << 10, 1 << 30)):
+    for B, T in ((0, 4), (4, 0), (-1, 4), (1 << 19, 4), (1 << 10, 1 << 30), (1, (1 << 30) + 1)):
         assert lib.deer_linattn_workspace_bytes(ctypes.byref(s), B, T, _b.DEER_OP_SOLVE) == 0, (B, T)
     assert lib.deer_linattn_workspace_bytes(ctypes.byref(s), 2, 16, _b.DEER_OP_JACOBIAN) == 0
     assert lib.deer_linattn_workspace_bytes(None, 2, 16, _b.DEER_OP_SOLVE) == 0
@@ -71,7 +71,7 @@ def test_forward_arguments(lib):
     for x in ("q", "k", "v", "ld", "o"):
         assert _forward(lib, s, **{x: None}) == BAD, x
     assert _forward(lib, s, q=_view(None)) == BAD
-    for st in (dict(sb=-1), dict(st=-1), dict(sh=-8)):
+    for st in (dict(sb=-1), dict(st=-1), dict(sh=-8), dict(st=(1 << 22) + 1)):
         assert _forward(lib, s, v=_view(P[2], **st)) == BAD and b"stride" in lib.deer_last_error()
     for o in (0, 1, 2, 4, 7):
         assert _forward(lib, s, o=o, state0=7) == BAD and b"input" in lib.deer_last_error()
