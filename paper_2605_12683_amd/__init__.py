@@ -443,13 +443,13 @@ def deer_noalloc_scratch_bytes() -> int:
 _DTYPES = {torch.float32: _b.DEER_F32, torch.bfloat16: _b.DEER_BF16, torch.float16: _b.DEER_F16}
 
 
-def _operand(name, t, ref=None, shape=None, dtype=None):
-    """Checks an argument of a layer (a GPU tensor on ref's GPU, of the given shape and type)."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+def _operand(name, t, gpu=None, shape=None, dtype=None):
+    """Checks an argument of a layer: a GPU tensor, on the GPU of that index, of the given shape and type."""
+    if not isinstance(t, torch.Tensor) or t.get_device() < 0:
         raise ValueError(f"{name} must be a GPU tensor")
-    if ref is not None and t.device != ref.device:
-        raise ValueError(f"{name} is on {t.device}, not on {ref.device}")
-    if dtype is not None and t.dtype != dtype:
+    if gpu is not None and t.get_device() != gpu:
+        raise ValueError(f"{name} is on {t.device}, not on cuda:{gpu}")
+    if dtype is not None and t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
     if shape is not None and t.shape != shape:
         raise ValueError(f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
@@ -465,18 +465,31 @@ def _at(t):
     return None if t is None else t.data_ptr()
 
 
-def _on(t):
-    """Makes t's GPU the current one (nothing to do if it is)."""
-    return contextlib.nullcontext() if torch.cuda.current_device() == t.device.index else torch.cuda.device(t.device)
+_already = contextlib.nullcontext()
 
 
-def _result(name, t, ref, shape, dtype):
-    """A caller's output buffer, or a new one."""
+def _on(gpu):
+    """Makes a GPU the current one (nothing to do if it is)."""
+    return _already if torch.cuda.current_device() == gpu else torch.cuda.device(gpu)
+
+
+def _result(name, t, gpu, shape, dtype):
+    """A caller's output buffer, or a new one on the current GPU, which is that of index gpu."""
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=ref.device)
-    if not _operand(name, t, ref, shape, dtype).is_contiguous():
+        return torch.empty(shape, dtype=dtype, device="cuda")
+    if not _operand(name, t, gpu, shape, dtype).is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t
+
+
+def _scratch(ws, gpu, need):
+    """A caller's workspace, or a new one, and its size in bytes."""
+    if ws is None:
+        ws = torch.empty(need or 256, dtype=torch.uint8, device="cuda")
+        return ws, ws.numel()
+    if not _operand("ws", ws, gpu).is_contiguous():
+        raise ValueError("ws must be contiguous")
+    return ws, ws.numel() * ws.element_size()
 
 
 def _view(t):
@@ -488,41 +501,41 @@ def _view(t):
 
 
 class _Lin:
-    """The checked operands of one call of linear attention."""
+    """The checked operands of one call of linear attention over sequences (dim = 4) or of one step (3)."""
 
-    def __init__(self, q, k, v, log_decay, scale, lengths):
-        dim = _operand("v", v).dim()
-        if dim not in (3, 4):
-            raise ValueError("v must be [B, T, H, Dv] (a step: [B, H, Dv])")
-        if v.dtype not in _DTYPES:
-            raise ValueError(f"unsupported type {v.dtype}")
-        if _operand("q", q, v, None, v.dtype).dim() != dim:
-            raise ValueError("q must have as many dimensions as v")
-        lead = tuple(v.shape[:-2])
-        self.H, self.Dv = v.shape[-2:]
-        self.Hk, self.Dk = q.shape[-2:]
-        self.lead = lead
-        self.B, self.T = lead[0], lead[1] if dim == 4 else 1
-        _operand("q", q, v, (*lead, self.Hk, self.Dk))
-        _operand("k", k, v, (*lead, self.Hk, self.Dk), v.dtype)
-        _operand("log_decay", log_decay, v, None, torch.float32)
-        per_step = log_decay.dim() > 1
-        _operand("log_decay", log_decay, v, (*lead, self.H) if per_step else (self.H,))
+    def __init__(self, dim, q, k, v, log_decay, scale, lengths):
+        if _operand("v", v).dim() != dim:
+            raise ValueError("v must be [B, T, H, Dv]" if dim == 4 else "v must be [B, H, Dv]")
+        dtype, gpu = v.dtype, v.get_device()
+        if dtype not in _DTYPES:
+            raise ValueError(f"unsupported type {dtype}")
+        *lead, H, Dv = v.shape
+        if max(v.shape) >> 31:
+            raise ValueError(f"a dimension of 2^31 or more: {tuple(v.shape)}")
+        _operand("k", k, gpu, None, dtype)
+        if _operand("q", q, gpu, k.shape, dtype).dim() != dim or list(q.shape[:-2]) != lead:
+            raise ValueError(f"q must be {lead} by heads by Dk, not {tuple(q.shape)}")
+        Hk, Dk = q.shape[-2:]
+        if max(Hk, Dk) >> 31:
+            raise ValueError(f"a dimension of 2^31 or more: {tuple(q.shape)}")
+        per_step = _operand("log_decay", log_decay, gpu, None, torch.float32).dim() > 1
+        _operand("log_decay", log_decay, gpu, (*lead, H) if per_step else (H,))
         if lengths is not None:
-            lengths = _operand("lengths", lengths, v, (self.B,), torch.int32).contiguous()
+            lengths = _operand("lengths", lengths, gpu, (lead[0],), torch.int32).contiguous()
+        self.gpu, self.B, self.T, self.shape = gpu, lead[0], lead[1] if dim == 4 else 1, (lead[0], H, Dk, Dv)
         (self.q, self.vq), (self.k, self.vk), (self.v, self.vv) = _view(q), _view(k), _view(v)
         self.log_decay, self.lengths = log_decay.contiguous(), lengths
-        self.c = _b.deer_linattn_shape(_DTYPES[v.dtype], self.H, self.Hk, self.Dk, self.Dv, int(per_step), float(scale))
+        self.c = _b.deer_linattn_shape(_DTYPES[dtype], H, Hk, Dk, Dv, per_step, float(scale))
 
     def matrix(self, name, t):
         """A state or its cotangent, contiguous."""
         if t is None:
             return None
-        return _operand(name, t, self.v, (self.B, self.H, self.Dk, self.Dv), torch.float32).contiguous()
+        return _operand(name, t, self.gpu, self.shape, torch.float32).contiguous()
 
-    def workspace(self, lib, op):
-        n = lib.deer_linattn_workspace_bytes(ctypes.byref(self.c), self.B, self.T, op)
-        return torch.empty(max(int(n), 256), dtype=torch.uint8, device=self.v.device)
+    def scratch(self, lib, ws, op):
+        need = 0 if ws is not None else lib.deer_linattn_workspace_bytes(ctypes.byref(self.c), self.B, self.T, op)
+        return _scratch(ws, self.gpu, need)
 
 
 def deer_linattn_workspace_bytes(B: int, T: int, H: int, Hk: int, Dk: int, Dv: int, op: int,
@@ -544,19 +557,16 @@ def deer_linattn(q, k, v, log_decay, *, scale: float = 1.0, lengths=None, state0
     state0 float32 [B, H, Dk, Dv].  o and state are buffers for the outputs; state may be state0.
     Returns dict(o [B, T, H, Dv], state (None unless want_state or a buffer is given))."""
     lib = load()
-    a = _Lin(q, k, v, log_decay, scale, lengths)
-    if v.dim() != 4:
-        raise ValueError("v must be [B, T, H, Dv]")
-    with _on(v):
-        o = _result("o", o, v, a.v.shape, v.dtype)
+    a = _Lin(4, q, k, v, log_decay, scale, lengths)
+    with _on(a.gpu):
+        o = _result("o", o, a.gpu, v.shape, v.dtype)
         s0 = a.matrix("state0", state0)
         if state is not None or want_state:
-            state = _result("state", state, v, (a.B, a.H, a.Dk, a.Dv), torch.float32)
-        if ws is None:
-            ws = a.workspace(lib, _b.DEER_OP_SOLVE)
+            state = _result("state", state, a.gpu, a.shape, torch.float32)
+        ws, ws_bytes = a.scratch(lib, ws, _b.DEER_OP_SOLVE)
         st = lib.deer_linattn(ctypes.byref(a.c), a.B, a.T, ctypes.byref(a.vq), ctypes.byref(a.vk), ctypes.byref(a.vv),
-                              _at(a.log_decay), _at(a.lengths), _at(s0), _at(o), _at(state), _at(ws), ws.numel(),
-                              _raw_stream(v.device.index))
+                              _at(a.log_decay), _at(a.lengths), _at(s0), _at(o), _at(state), _at(ws), ws_bytes,
+                              _raw_stream(a.gpu))
     _b._check(st, "deer_linattn")
     return {"o": o, "state": state}
 
@@ -567,26 +577,21 @@ def deer_linattn_adjoint(q, k, v, log_decay, g, *, scale: float = 1.0, lengths=N
     (float32 [B, H, Dk, Dv] or None).  Returns dict(grads = {q, k, v, log_decay (with want_decay),
     state0 (if state0 is given)}); q, k, v in the operands' type, the others in float32."""
     lib = load()
-    a = _Lin(q, k, v, log_decay, scale, lengths)
-    if v.dim() != 4:
-        raise ValueError("v must be [B, T, H, Dv]")
-    with _on(v):
-        gt, vg = _view(_operand("g", g, v, v.shape, v.dtype))
+    a = _Lin(4, q, k, v, log_decay, scale, lengths)
+    with _on(a.gpu):
+        gt, vg = _view(_operand("g", g, a.gpu, v.shape, v.dtype))
         s0, gs = a.matrix("state0", state0), a.matrix("g_state", g_state)
-        grads = {"q": torch.empty(q.shape, dtype=q.dtype, device=v.device),
-                 "k": torch.empty(k.shape, dtype=k.dtype, device=v.device),
-                 "v": torch.empty(v.shape, dtype=v.dtype, device=v.device)}
+        grads = {n: torch.empty(x.shape, dtype=x.dtype, device="cuda") for n, x in (("q", q), ("k", k), ("v", v))}
         if want_decay:
-            grads["log_decay"] = torch.empty(log_decay.shape, device=v.device)
+            grads["log_decay"] = torch.empty(log_decay.shape, dtype=torch.float32, device="cuda")
         if s0 is not None:
-            grads["state0"] = torch.empty(s0.shape, device=v.device)
-        if ws is None:
-            ws = a.workspace(lib, _b.DEER_OP_ADJOINT)
+            grads["state0"] = torch.empty(a.shape, dtype=torch.float32, device="cuda")
+        ws, ws_bytes = a.scratch(lib, ws, _b.DEER_OP_ADJOINT)
         st = lib.deer_linattn_adjoint(ctypes.byref(a.c), a.B, a.T, ctypes.byref(a.vq), ctypes.byref(a.vk),
                                       ctypes.byref(a.vv), _at(a.log_decay), _at(a.lengths), _at(s0),
                                       ctypes.byref(vg), _at(gs), _at(grads["q"]), _at(grads["k"]), _at(grads["v"]),
-                                      _at(grads.get("log_decay")), _at(grads.get("state0")), _at(ws), ws.numel(),
-                                      _raw_stream(v.device.index))
+                                      _at(grads.get("log_decay")), _at(grads.get("state0")), _at(ws), ws_bytes,
+                                      _raw_stream(a.gpu))
     _b._check(st, "deer_linattn_adjoint")
     return {"grads": grads}
 
@@ -596,42 +601,41 @@ def deer_linattn_step(q, k, v, log_decay, state, *, scale: float = 1.0, lengths=
     log_decay [H] or [B, H]; state float32 [B, H, Dk, Dv], contiguous, is updated in place.  A sequence
     whose entry of lengths (int32 [B]) is 0 takes no step.  Returns dict(o [B, H, Dv], state)."""
     lib = load()
-    a = _Lin(q, k, v, log_decay, scale, lengths)
-    if v.dim() != 3:
-        raise ValueError("v must be [B, H, Dv]")
-    with _on(v):
-        state = _result("state", _operand("state", state), v, (a.B, a.H, a.Dk, a.Dv), torch.float32)
-        o = _result("o", o, v, a.v.shape, v.dtype)
+    a = _Lin(3, q, k, v, log_decay, scale, lengths)
+    with _on(a.gpu):
+        state = _result("state", _operand("state", state), a.gpu, a.shape, torch.float32)
+        o = _result("o", o, a.gpu, v.shape, v.dtype)
         st = lib.deer_linattn_step(ctypes.byref(a.c), a.B, ctypes.byref(a.vq), ctypes.byref(a.vk), ctypes.byref(a.vv),
-                                   _at(a.log_decay), _at(a.lengths), _at(state), _at(o), _raw_stream(v.device.index))
+                                   _at(a.log_decay), _at(a.lengths), _at(state), _at(o), _raw_stream(a.gpu))
     _b._check(st, "deer_linattn_step")
     return {"o": o, "state": state}
 
 
 def _norm(x, w, b, eps):
-    """Contiguous x, w, b, the row count and the C struct: weights [D], or [G, D] for x [..., G, D]."""
-    _operand("x", x)
+    """The GPU, contiguous x, w, b, the row count and the C struct: weights [D], or [G, D] for x [..., G, D]."""
+    gpu = _operand("x", x).get_device()
     if x.dtype not in _DTYPES:
         raise ValueError(f"unsupported type {x.dtype}")
     if x.dim() < 1:
         raise ValueError("x must have at least one dimension")
-    given = w if w is not None else b
     G, wtype = 1, _b.DEER_F32
+    given = b if w is None else w
     if given is not None:
-        _operand("w" if w is not None else "b", given, x)
-        if given.dtype not in (torch.float32, x.dtype):
+        n = _operand("b" if w is None else "w", given, gpu).dim()
+        if given.dtype is not torch.float32 and given.dtype is not x.dtype:
             raise ValueError(f"w and b must be float32 or {x.dtype}, not {given.dtype}")
-        if given.dim() not in (1, 2) or tuple(given.shape) != tuple(x.shape[x.dim() - given.dim():]):
+        if n not in (1, 2) or given.shape != x.shape[-n:]:
             raise ValueError(f"w and b must have the shape of x's last or last two dimensions, not {tuple(given.shape)}")
-        if b is not None:
-            _operand("b", b, x, given.shape, given.dtype)
-        G = given.shape[0] if given.dim() == 2 else 1
-        wtype = _DTYPES[given.dtype]
+        if w is not None and b is not None:
+            _operand("b", b, gpu, w.shape, w.dtype)
+        G, wtype = given.shape[0] if n == 2 else 1, _DTYPES[given.dtype]
+        w, b = (None if t is None else t.contiguous() for t in (w, b))
     x = x.contiguous()
-    w, b = (None if t is None else t.contiguous() for t in (w, b))
     D = x.shape[-1]
+    if max(G, D) >> 31:
+        raise ValueError(f"a row or a number of groups of 2^31 or more: {tuple(x.shape)}")
     rows = x.numel() // D if D else 0
-    return x, w, b, rows, _b.deer_norm(_DTYPES[x.dtype], wtype, G, D, _at(w), _at(b), float(eps))
+    return gpu, x, w, b, rows, _b.deer_norm(_DTYPES[x.dtype], wtype, G, D, _at(w), _at(b), float(eps))
 
 
 def deer_layernorm_workspace_bytes(rows: int, G: int, D: int, dtype=torch.float32) -> int:
@@ -645,12 +649,12 @@ def deer_layernorm(x, w=None, b=None, *, eps: float = 1e-5, y=None) -> dict:
     y = (x - mean) rstd w + b.  w, b: [D], or [G, D] with x [..., G, D] (weights of its own for each
     head), float32 or x's type, or None.  Returns dict(y, mean, rstd), the statistics in float32."""
     lib = load()
-    xc, wc, bc, rows, c = _norm(x, w, b, eps)
-    with _on(x):
-        y = _result("y", y, x, x.shape, x.dtype)
-        mean = torch.empty(x.shape[:-1], device=x.device)
-        rstd = torch.empty(x.shape[:-1], device=x.device)
-        st = lib.deer_layernorm(ctypes.byref(c), rows, _at(xc), _at(y), _at(mean), _at(rstd), _raw_stream(x.device.index))
+    gpu, xc, wc, bc, rows, c = _norm(x, w, b, eps)
+    with _on(gpu):
+        y = _result("y", y, gpu, x.shape, x.dtype)
+        mean = torch.empty(x.shape[:-1], dtype=torch.float32, device="cuda")
+        rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device="cuda")
+        st = lib.deer_layernorm(ctypes.byref(c), rows, _at(xc), _at(y), _at(mean), _at(rstd), _raw_stream(gpu))
     _b._check(st, "deer_layernorm")
     return {"y": y, "mean": mean, "rstd": rstd}
 
@@ -659,20 +663,18 @@ def deer_layernorm_adjoint(x, g, mean, rstd, w=None, *, want_grads: bool = True,
     """Gradients of deer_layernorm for the cotangent g of y, with its mean and rstd.  Returns dict(x =
     dL/dx in x's type, grads = {w, b} in float32, of w's shape ([D] without w); {} without want_grads)."""
     lib = load()
-    xc, wc, _, rows, c = _norm(x, w, None, 0.0)
-    with _on(x):
-        gc = _operand("g", g, x, x.shape, x.dtype).contiguous()
-        mc = _operand("mean", mean, x, x.shape[:-1], torch.float32).contiguous()
-        rc = _operand("rstd", rstd, x, x.shape[:-1], torch.float32).contiguous()
-        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    gpu, xc, wc, _, rows, c = _norm(x, w, None, 0.0)
+    with _on(gpu):
+        gc = _operand("g", g, gpu, x.shape, x.dtype).contiguous()
+        mc = _operand("mean", mean, gpu, x.shape[:-1], torch.float32).contiguous()
+        rc = _operand("rstd", rstd, gpu, x.shape[:-1], torch.float32).contiguous()
+        dx = torch.empty(x.shape, dtype=x.dtype, device="cuda")
         grads = {}
         if want_grads:
             shape = x.shape[-1:] if w is None else w.shape
-            grads = {"w": torch.empty(shape, device=x.device), "b": torch.empty(shape, device=x.device)}
-        if ws is None:
-            n = lib.deer_layernorm_workspace_bytes(ctypes.byref(c), rows)
-            ws = torch.empty(max(int(n), 256), dtype=torch.uint8, device=x.device)
+            grads = {n: torch.empty(shape, dtype=torch.float32, device="cuda") for n in ("w", "b")}
+        ws, ws_bytes = _scratch(ws, gpu, 0 if ws is not None else lib.deer_layernorm_workspace_bytes(ctypes.byref(c), rows))
         st = lib.deer_layernorm_adjoint(ctypes.byref(c), rows, _at(xc), _at(gc), _at(mc), _at(rc), _at(dx),
-                                        _at(grads.get("w")), _at(grads.get("b")), _at(ws), ws.numel(), _raw_stream(x.device.index))
+                                        _at(grads.get("w")), _at(grads.get("b")), _at(ws), ws_bytes, _raw_stream(gpu))
     _b._check(st, "deer_layernorm_adjoint")
     return {"x": dx, "grads": grads}

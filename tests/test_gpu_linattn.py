@@ -428,6 +428,11 @@ def test_refusals():
         D.deer_linattn(**c, scale=float("nan"))
     with pytest.raises(D.DeerError):
         D.deer_linattn(**c, ws=torch.empty(0, dtype=torch.uint8, device="cuda"))
+    for ws in (torch.empty(1 << 20, dtype=torch.uint8), torch.empty(2, 1 << 20, dtype=torch.uint8, device="cuda")[:, ::2]):
+        with pytest.raises(ValueError):
+            D.deer_linattn(**c, ws=ws)
+        with pytest.raises(ValueError):
+            D.deer_linattn_adjoint(**c, g=g, ws=ws)
     step = {n: x[:, 0] for n, x in c.items()}
     with pytest.raises(ValueError):
         D.deer_linattn_step(**step, state=gs.transpose(-1, -2))
