@@ -88,7 +88,9 @@ template <int NPI, int KT, int NW, int CT, int NPX, int MODE>   // waves, 16-col
 struct LinTile {
     static constexpr bool OUT = MODE != kStates;
     static constexpr int NB = 16 * NW * CT, TH = 64 * NW;
-    static constexpr int PQ = KT + 8, PK = KT + 16, PV = NB + 16;   // LDS row pitches: no bank conflicts
+    // LDS row pitches, in which neither rows read 8 or 4 elements a lane nor rows read across meet in
+    // a bank (for 4 elements a lane: with k's columns of each 16 swapped by halves in rows 8..15 of 16)
+    static constexpr int PQ = KT + 16, PK = KT + 16, PV = NB + 16;
     static constexpr int pairs(int C) { return C == 64 ? 6 : 2; }   // (16 outputs, 32 sources) not all above the diagonal
     static constexpr int bytes(int C) {
         return NPI * C * 2 * ((OUT ? PQ : 0) + PK + PV) + (OUT ? pairs(C) * NPX * 1024 : 0) + 2 * (4 * C + 4) * 4 +
@@ -173,8 +175,9 @@ struct RowTile {
         }
     }
 
-    // planes of bf16 parts [C][pitch]; PERM: the columns of each 32 in the order 4 g + 0..3, 16 + 4 g + 0..3
-    template <bool PERM>
+    // planes of bf16 parts [C][pitch]; PERM: the columns of each 32 in the order 4 g + 0..3, 16 + 4 g + 0..3;
+    // SWAP: the columns of each 16 swapped by halves in every other eight rows
+    template <bool PERM, bool SWAP>
     __device__ __forceinline__ void store(uint16_t *lds, int pitch) const {
         constexpr int NP = InParts<Ty>::n;
         const int tid = afresh((int)threadIdx.x);
@@ -182,8 +185,9 @@ struct RowTile {
         for (int i = 0; i < NU; ++i) {
             const int n = i * TH + tid, row = n / UPR, d = (n % UPR) * E;
             if (C * UPR % TH != 0 && row >= C) continue;
+            const int swap = SWAP ? row & 8 : 0;
             if constexpr (NP == 1 && !PERM) {
-                *(v4u *)(lds + row * pitch + d) = u[i];
+                *(v4u *)(lds + row * pitch + (d ^ swap)) = u[i];
                 continue;
             }
 #pragma unroll
@@ -191,7 +195,7 @@ struct RowTile {
                 uint32_t p[NP][2];
                 parts(u[i], half, p);
                 const int e = d + 4 * half;
-                const int at = PERM ? (e & ~31) + ((e & 15) >> 2) * 8 + ((e >> 4) & 1) * 4 : e;
+                const int at = PERM ? (e & ~31) + ((e & 15) >> 2) * 8 + ((e >> 4) & 1) * 4 : e ^ swap;
 #pragma unroll
                 for (int q = 0; q < NP; ++q)
                     *(v2u *)(lds + (q * C + row) * pitch + at) = v2u{p[q][0], p[q][1]};
@@ -449,13 +453,13 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
                        ro.partner.st >= N;
     }
 
-    // tiles above the diagonal that share an operand with one on it stay zero
-    if constexpr (OUT)
+    // the tile above the diagonal that shares an operand with the first stays zero
+    if constexpr (OUT && C == 32)
         for (int i = threadIdx.x; i < PAIRS * NPX * 64; i += TH) Ps[i] = v4u{0, 0, 0, 0};
     auto store = [&] {
-        kr.template store<false>(Ks, PK);
-        vr.template store<false>(Vs, PV);
-        if constexpr (OUT) qr.template store<true>(Qs, PQ);
+        kr.template store<false, OUT>(Ks, PK);
+        vr.template store<false, false>(Vs, PV);
+        if constexpr (OUT) qr.template store<true, false>(Qs, PQ);
     };
     double total = 0.0, ls = 0.0;                              // last wave: log2 decay of the segment, the registers' scale
     float raw = 0.f;
@@ -496,21 +500,23 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
 
         v4f O[NT][CT];
         if constexpr (OUT) {
-            // decayed scores, transposed (rows j, columns i): tiles w, w + NW, ... of those on and below
-            // the diagonal, a wave's tiles side by side so that their latencies overlap
-            constexpr int TRI = NT * (NT + 1) / 2, MOST = (TRI + NW - 1) / NW;
+            // decayed scores, transposed (rows j, columns i), in tiles of those on and below the diagonal.
+            // C = 32: one tile for each of the first three waves.  C = 64: two tiles of one row for each
+            // wave, which share its q, and for waves 0 and 1 the first tile of row 2 w.
+            constexpr bool TWO = C == 64;
+            static_assert(!TWO || NW == 4, "");
             auto scores = [&](auto count) {
                 constexpr int M = decltype(count)::value;
                 const int lane = lane_now(), g = lane >> 4, c = lane & 15;
                 int it[M], jt[M];
+                it[0] = TWO ? (w < 3 ? w + 1 : 3) : (w + 1) / 2;
+                jt[0] = TWO ? (w < 3 ? 0 : 2) : w / 2;
+                if constexpr (M > 1) it[1] = it[0], jt[1] = jt[0] + 1;
+                if constexpr (M > 2) it[2] = jt[2] = 2 * w;
                 float hi_i[M], lo_i[M];
                 v4f hi_j[M], lo_j[M], acc[M];
 #pragma unroll
-                for (int m = 0; m < M; ++m) {
-                    const int tl = w + m * NW;
-                    it[m] = tl >= 6 ? 3 : tl >= 3 ? 2 : tl >= 1 ? 1 : 0, jt[m] = tl - it[m] * (it[m] + 1) / 2;
-                    acc[m] = v4f{0.f, 0.f, 0.f, 0.f};
-                }
+                for (int m = 0; m < M; ++m) acc[m] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int u0 = 0; u0 < KT / 32; u0 += UB) {
                     v4u kf[M][UB][NPI], qf[M][UB][NPI];
@@ -520,10 +526,10 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
                         for (int u = 0; u < UB; ++u)
 #pragma unroll
                             for (int p = 0; p < NPI; ++p) {
-                                const uint16_t *kp = Ks + (p * C + jt[m] * 16 + c) * PK + (u0 + u) * 32 + 4 * g;
+                                const uint16_t *kp = Ks + (p * C + jt[m] * 16 + c) * PK + (u0 + u) * 32 + (4 * g ^ (c & 8));
                                 const v2u k0 = *(const v2u *)kp, k1 = *(const v2u *)(kp + 16);
                                 kf[m][u][p] = v4u{k0[0], k0[1], k1[0], k1[1]};
-                                qf[m][u][p] = *(const v4u *)(Qs + (p * C + it[m] * 16 + c) * PQ + (u0 + u) * 32 + 8 * g);
+                                if (m != 1) qf[m][u][p] = *(const v4u *)(Qs + (p * C + it[m] * 16 + c) * PQ + (u0 + u) * 32 + 8 * g);
                             }
                     if (u0 + UB >= KT / 32)
 #pragma unroll
@@ -536,8 +542,9 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
 #pragma unroll
                     for (int u = 0; u < UB; ++u)
 #pragma unroll
-                        for (int m = 0; m < M; ++m) acc[m] = mfma_parts<NPI - 1>(kf[m][u], qf[m][u], acc[m]);
+                        for (int m = 0; m < M; ++m) acc[m] = mfma_parts<NPI - 1>(kf[m][u], qf[m == 1 ? 0 : m][u], acc[m]);
                 }
+                uint32_t pp[M][2][3];
 #pragma unroll
                 for (int m = 0; m < M; ++m) {
                     const int above = it[m] == jt[m] ? 4 * g - c : -64;   // j - i of the first row, on the diagonal
@@ -548,16 +555,23 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
                         const float p = acc[m][r] * sc_p * __builtin_amdgcn_exp2f(e);
                         x[r] = above + r <= 0 ? p : 0.f;
                     }
-                    uint32_t *dst = (uint32_t *)(Ps + pair(it[m], jt[m] >> 1) * NPX * 64 + lane) + (jt[m] & 1) * 2;
-                    uint32_t p0[3], p1[3];
-                    split_pair(x[0], x[1], p0);
-                    split_pair(x[2], x[3], p1);
+                    split_pair(x[0], x[1], pp[m][0]);
+                    split_pair(x[2], x[3], pp[m][1]);
+                }
+                auto operand = [&](int m) { return Ps + pair(it[m], jt[m] >> 1) * NPX * 64 + lane; };
 #pragma unroll
-                    for (int q = 0; q < NPX; ++q) *(v2u *)(dst + q * 64 * 4) = v2u{p0[q], p1[q]};
+                for (int q = 0; q < NPX; ++q) {
+                    if constexpr (TWO) operand(0)[q * 64] = v4u{pp[0][0][q], pp[0][1][q], pp[1][0][q], pp[1][1][q]};
+                    else *((v2u *)(operand(0) + q * 64) + (jt[0] & 1)) = v2u{pp[0][0][q], pp[0][1][q]};
+                    if constexpr (M > 2) operand(2)[q * 64] = v4u{pp[2][0][q], pp[2][1][q], 0, 0};   // (above the diagonal)
                 }
             };
-            if (w + (MOST - 1) * NW < TRI) scores(std::integral_constant<int, MOST>{});
-            else if constexpr (MOST > 1) scores(std::integral_constant<int, MOST - 1>{});
+            if constexpr (TWO) {
+                if (w < 2) scores(std::integral_constant<int, 3>{});
+                else scores(std::integral_constant<int, 2>{});
+            } else if (w < 3) {
+                scores(std::integral_constant<int, 1>{});
+            }
             if (ahead) vr.load(rows_ahead);
             // what the entering state gives, transposed: rows n, columns i
             const int lane = lane_now(), g = lane >> 4, c = lane & 15;
@@ -681,7 +695,8 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
                 for (int m = 0; m < KB; ++m)
 #pragma unroll
                     for (int p = 0; p < NPI; ++p) {
-                        const uint16_t *kp = Ks + p * C * PK + (ks * 32 + 4 * g + (c >> 2)) * PK + (n * KB + m) * 16 + 4 * (c & 3);
+                        const uint16_t *kp = Ks + p * C * PK + (ks * 32 + 4 * g + (c >> 2)) * PK + (n * KB + m) * 16 +
+                                             (4 * (c & 3) ^ (OUT ? (g >> 1) * 8 : 0));
                         const v2u k0 = read_turned(kp), k1 = read_turned(kp + 16 * PK);
                         kf[n & 1][m][p] = v4u{k0[0], k0[1], k1[0], k1[1]};
                     }
