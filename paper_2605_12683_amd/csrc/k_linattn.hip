@@ -24,7 +24,7 @@ __global__ __launch_bounds__(256) void k_lin_join(LinArgs a, LinRoles rs) {
     const int mat = ro.Kd * ro.N, per = (mat + 1023) / 1024;
     const int bh = blockIdx.x / per, e = (blockIdx.x % per * 256 + threadIdx.x) * 4;
     if (bh >= a.B * a.H || e >= mat) return;
-    const int b = bh / a.H, h = bh % a.H, left = mat - e < 4 ? mat - e : 4;
+    const int left = mat - e < 4 ? mat - e : 4;
     const bool four = mat % 4 == 0;
     float S[4] = {0.f, 0.f, 0.f, 0.f};
     if (ro.init)
@@ -40,7 +40,7 @@ __global__ __launch_bounds__(256) void k_lin_join(LinArgs a, LinRoles rs) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int i = i0 + u, s = ro.reverse ? a.nseg - 1 - i : i;
-            const bool on = i < a.nseg - 1 || (i == a.nseg - 1 && ro.fin);
+            const bool on = i < a.nseg - 1;
             const float *p = seg + (size_t)s * mat;
             v4f y = {0.f, 0.f, 0.f, 0.f};
             if (on && four) y = *(const v4f *)p;
@@ -61,12 +61,6 @@ __global__ __launch_bounds__(256) void k_lin_join(LinArgs a, LinRoles rs) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) S[r] = fmaf(f[u], S[r], x[u][r]);
         }
-    }
-    if (!ro.fin) return;
-    const float f = ro.reverse ? __builtin_amdgcn_exp2f((float)gate_of(gate_raw(a, b, h, -1, length_of(a, b), true))) : 1.f;
-    for (int r = 0; r < left; ++r) {
-        const int d = (e + r) / ro.N, n = (e + r) % ro.N;
-        ro.fin[(size_t)bh * mat + (size_t)d * ro.fin_d + (size_t)n * ro.fin_n] = f * S[r];
     }
 }
 

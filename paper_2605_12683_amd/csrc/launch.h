@@ -350,8 +350,8 @@ struct LinRole {
     float *dot;                 // [tiles][B, H, T]
     float *anchor;              // [B, H, anchors][Kd, N] or null: the state at every kLinAnchor steps
     bool wide_out;              // N is a multiple of 8 and out lies on 16 bytes
-    // walks in segments: first what each segment adds by itself, then (joined) the state entering
-    // each: [B, H, segments] matrices, element (d, n) at d seg_d + n seg_n, and the segments' decays
+    // walks in segments: what each but the last adds by itself, or (joined) the state entering each:
+    // [B, H, segments] matrices, element (d, n) at d seg_d + n seg_n, and the segments' decays
     float *seg, *seg_decay;
     int seg_d, seg_n;
 };
@@ -362,6 +362,7 @@ struct LinArgs {
     bool per_step;
     const int32_t *lengths;     // [B] or null
     int seg_steps, nseg;        // segments of seg_steps steps (a multiple of 64), or one of all T
+    bool joined;                // seg holds the state entering each segment, not what each adds
 };
 int lin_tiles(int Kd, int N);   // blocks that share the N columns of one head's state
 bool lin_same_tile(int Kd, int N, int Kd2, int N2);
@@ -369,7 +370,7 @@ bool lin_same_tile(int Kd, int N, int Kd2, int N2);
 // seg_decay), else the outputs; dots: and dot, anchor (which are summed over many steps, so the
 // intermediate values of 16-bit operands then take 24 bits, not 16)
 int launch_lin_walk(const LinArgs &a, const LinRole *roles, int nroles, bool states, bool dots, hipStream_t st);
-// seg from what each segment adds to the state entering it; fin
+// seg from what each segment adds to the state entering it
 int launch_lin_join(const LinArgs &a, const LinRole *roles, int nroles, hipStream_t st);
 int launch_lin_walk_bf16(const LinArgs &a, const LinRole *roles, int n, bool states, bool dots, hipStream_t st);
 int launch_lin_walk_f16(const LinArgs &a, const LinRole *roles, int n, bool states, bool dots, hipStream_t st);

@@ -178,27 +178,30 @@ struct RowTile {
     // planes of bf16 parts [C][pitch]; PERM: the columns of each 32 in the order 4 g + 0..3, 16 + 4 g + 0..3;
     // SWAP: the columns of each 16 swapped by halves in every other eight rows
     template <bool PERM, bool SWAP>
-    __device__ __forceinline__ void store(uint16_t *lds, int pitch) const {
+    __device__ __forceinline__ void store(uint16_t *lds, const int pitch) const {
         constexpr int NP = InParts<Ty>::n;
-        const int tid = afresh((int)threadIdx.x);
+        static_assert(TH % UPR == 0 && (ROWS & (ROWS - 1)) == 0, "");
+        // everything that depends on the thread stands outside the loop: its units are ROWS rows apart
+        const uint32_t tid = (uint32_t)afresh((int)threadIdx.x), row0 = tid / UPR, d = tid % UPR * E;
+        const uint32_t swap0 = SWAP ? row0 & 8 : 0;
+        lds += row0 * pitch;
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
-            const int n = i * TH + tid, row = n / UPR, d = (n % UPR) * E;
-            if (C * UPR % TH != 0 && row >= C) continue;
-            const int swap = SWAP ? row & 8 : 0;
+            if (C * UPR % TH != 0 && i * ROWS + row0 >= C) continue;
+            const uint32_t swap = SWAP ? swap0 ^ (i * ROWS & 8) : 0;
             if constexpr (NP == 1 && !PERM) {
-                *(v4u *)(lds + row * pitch + (d ^ swap)) = u[i];
+                *(v4u *)(lds + i * ROWS * pitch + (d ^ swap)) = u[i];
                 continue;
             }
 #pragma unroll
             for (int half = 0; half < E / 4; ++half) {   // four elements at a time
                 uint32_t p[NP][2];
                 parts(u[i], half, p);
-                const int e = d + 4 * half;
-                const int at = PERM ? (e & ~31) + ((e & 15) >> 2) * 8 + ((e >> 4) & 1) * 4 : e ^ swap;
+                const uint32_t e = d + 4 * half;
+                const uint32_t at = PERM ? (e & ~31) + ((e & 15) >> 2) * 8 + ((e >> 4) & 1) * 4 : e ^ swap;
 #pragma unroll
                 for (int q = 0; q < NP; ++q)
-                    *(v2u *)(lds + (q * C + row) * pitch + at) = v2u{p[q][0], p[q][1]};
+                    *(v2u *)(lds + (q * C + i * ROWS) * pitch + at) = v2u{p[q][0], p[q][1]};
             }
         }
     }
@@ -380,8 +383,8 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
     const size_t mat = (size_t)Kd * N;
     const int col0 = tile * NB, n0 = col0 + w * 16 * CT;       // the block's and the wave's first column
 
-    // the segment that comes last adds to no other: its own sum is needed for the last state only
-    if (!OUT && seg == (rev ? 0 : a.nseg - 1) && !ro.fin) return;
+    const bool last = seg == (rev ? 0 : a.nseg - 1);           // in the walk's order
+    if (!OUT && last) return;                                  // adds to no other
 
     auto t0_of = [&](int n) { return lo + (rev ? chunks - 1 - n : n) * C; };
     RowTile<Ty, C, KT, TH> qr, kr;
@@ -409,20 +412,28 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
         return d < Kd && n < N ? (uint32_t)(d * sd + n * sn) * 4u : kOutside;
     };
     {
-        const float *src = nullptr;
-        int sd = 0, sn = 0;
-        if (OUT) {
-            if (a.nseg > 1) src = ro.seg + ((size_t)bh * a.nseg + seg) * mat, sd = ro.seg_d, sn = ro.seg_n;
-            else if (ro.init) src = ro.init + bh * mat, sd = ro.init_d, sn = ro.init_n;
-        }
-        const auto rsrc = bounded_rsrc(src, src ? (uint32_t)(mat * 4) : 0u);
         const int l = threadIdx.x & 63;
+        auto add_to = [&](float f, const float *src, int sd, int sn) {   // S = f S + src
+            const auto rsrc = bounded_rsrc(src, src ? (uint32_t)(mat * 4) : 0u);
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) S[dt][ct][r] = fmaf(f, S[dt][ct][r], bload(rsrc, at(l, dt, ct, r, sd, sn), 0));
+        };
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) S[dt][ct][r] = bload(rsrc, at(l, dt, ct, r, sd, sn), 0);
+            for (int ct = 0; ct < CT; ++ct) S[dt][ct] = v4f{0.f, 0.f, 0.f, 0.f};
+        if constexpr (OUT) {
+            const float *own = ro.seg + ((size_t)bh * a.nseg + seg) * mat;
+            if (a.joined) add_to(0.f, own, ro.seg_d, ro.seg_n);
+            else add_to(0.f, ro.init ? ro.init + bh * mat : nullptr, ro.init_d, ro.init_n);
+            if (!a.joined)                                     // the segments before this one
+                for (int s = rev ? a.nseg - 1 : 0; s != seg; s += rev ? -1 : 1)
+                    add_to(ro.seg_decay[(size_t)bh * a.nseg + s], own + ((long)s - seg) * (long)mat, ro.seg_d, ro.seg_n);
+        }
     }
     auto put_state = [&](float *dst, int sd, int sn, float f) {
         const auto rsrc = bounded_rsrc(dst, (uint32_t)(mat * 4));
@@ -470,7 +481,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
     }
     const int na = (a.T + kLinAnchor - 1) / kLinAnchor;
     const float sc_p = ro.sc_kv * ro.sc_o;
-    const bool keep = ro.fin && a.nseg == 1;                   // the state behind the last step is wanted
+    const bool keep = ro.fin && last;                          // the state behind the last step is wanted
     store();
 
     // The next chunk's rows are loaded while this one is computed and go to LDS before this one's
@@ -835,7 +846,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
     }
 
     if constexpr (OUT) {
-        if (ro.fin && a.nseg == 1) {
+        if (keep) {
             const float f = rev ? __builtin_amdgcn_exp2f((float)gate_of(gate_raw(a, b, h, -1, len, true))) : 1.f;
             put_state(ro.fin + bh * mat, ro.fin_d, ro.fin_n, f * dec[(chunks - 1) & 1].after);
         }

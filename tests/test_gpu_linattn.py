@@ -334,6 +334,17 @@ def test_prompt_then_steps(type_):
     check_forward(c, kw, {"o": torch.cat(outs, 1), "state": state})
 
 
+@pytest.mark.parametrize("seg", [64, 320])
+def test_state_in_place_over_segments(seg, monkeypatch):
+    """state0 overwritten by the state behind the last of 3 or 11 segments, which every block starts from."""
+    monkeypatch.setenv("DEER_LIN_SEG", str(seg))
+    c, kw, _, _ = make(2, 700, 8, 8, 128, 128, "bf16", state=True, lengths=[700, 300])
+    say("linattn in place over segments", seg)
+    state = kw["state0"].clone()
+    out = D.deer_linattn(**c, **{**kw, "state0": state}, state=state)
+    check_forward(c, kw, {"o": out["o"], "state": state})
+
+
 def test_gradients_against_differences():
     """Directional differences of the GPU's own forward pass: o and the state are linear in each of q,
     k, v and state0 alone; log_decay with a step whose square is below the tolerance."""
