@@ -59,20 +59,22 @@ static int seg_override() {
     return e ? atoi(e) : 0;
 }
 
-// Segments: enough that a walk's blocks fill the chip (two blocks share a CU, three of 64 columns),
-// none of fewer than kMinSeg steps; one where the heads alone give half of that, since segments read
-// k and v a second time.  (2 x 4096 steps, 16 heads of 128 x 128 in bf16, where one segment gives 32
-// blocks: segments of 256, 512, 1024, 4096 steps take 81, 79, 125, 304 us.)
+// Segments: as many as leave all blocks of a walk resident on the chip at once (a few blocks more
+// would run after the others, alone), none of fewer than kMinSeg steps; one where the heads alone give
+// half of that, since segments read k and v a second time.  (2 x 4096 steps, 16 heads of 128 x 128 in
+// bf16, where one segment gives 32 blocks of 512: segments of 256, 512, 1024, 4096 steps take 81, 83,
+// 123, 304 us.)
 constexpr int kMinSeg = 128;
 
 static int segment_steps(const deer_linattn_shape *s, int B, int T, int op) {
     if (const int n = seg_override(); n > 0) return n >= T ? T : (n + 63) / 64 * 64;
     // the adjoint's walks of dq and dk run together, that of dv by itself
     const bool adj = op == DEER_OP_ADJOINT;
-    const long blocks = (long)B * s->H * (adj ? 2 * lin_tiles(s->Dv, s->Dk) : lin_tiles(s->Dk, s->Dv));
-    const long fill = (adj ? s->Dk : s->Dv) <= 64 ? 768 : 512;
-    if (2 * blocks >= fill || T <= kMinSeg) return T;
-    const long n = (fill + blocks - 1) / blocks;
+    const int Kd = adj ? s->Dv : s->Dk, N = adj ? s->Dk : s->Dv;
+    const long blocks = (long)B * s->H * lin_tiles(Kd, N) * (adj ? 2 : 1);
+    const long fill = 256L * lin_resident(s->dtype, Kd, N, adj);
+    if (2 * blocks > fill || T <= kMinSeg) return T;
+    const long n = fill / blocks;
     const long steps = ((T + n - 1) / n + 63) / 64 * 64;
     return (int)(steps < kMinSeg ? kMinSeg : steps);
 }
@@ -269,11 +271,7 @@ int deer_linattn_adjoint(const deer_linattn_shape *s, int B, int T, const deer_v
     } else if ((rc = launch_lin_walk(a, ro, 2, false, decay, st)) || (rc = launch_lin_walk(a, ro + 2, 1, false, false, st))) {
         return rc;
     }
-    if (shared) {
-        const size_t rows = (size_t)B * T;
-        if ((rc = launch_lin_head_sum(s->dtype, rows, s->Hk, r, Dk, w.dq, dq, st))) return rc;
-        if ((rc = launch_lin_head_sum(s->dtype, rows, s->Hk, r, Dk, w.dk, dk, st))) return rc;
-    }
+    if (shared && (rc = launch_lin_head_sum(s->dtype, (size_t)B * T, s->Hk, r, Dk, w.dq, w.dk, dq, dk, st))) return rc;
     if (!decay) return DEER_OK;
     const int tiles = lin_tiles(Dv, Dk);
     return launch_lin_decay_grad(a, w.dq_dot, tiles, w.dk_dot, tiles, w.fwd, w.rev, Dk * Dv, w.part, dlog_decay, st);

@@ -83,6 +83,16 @@ int lin_tiles(int Kd, int N) {
     return (N + nb - 1) / nb;
 }
 
+int lin_resident(int dtype, int Kd, int N, bool dots) {
+    return with_dtype(dtype, [&](auto ty) {
+        constexpr int NPI = InParts<decltype(ty)>::n, NPX = NPI == 3 ? 3 : 2;
+        return with_walk_shape<NPI>(Kd, N, [&](auto s) {
+            return dots ? LinTile<NPI, s.KT, s.NW, s.CT, 3, kOutDots>::waves * 4 / s.NW
+                        : LinTile<NPI, s.KT, s.NW, s.CT, NPX, kOut>::waves * 4 / s.NW;
+        });
+    });
+}
+
 bool lin_same_tile(int Kd, int N, int Kd2, int N2) {
     return kt_of(Kd) == kt_of(Kd2) && nb_of(kt_of(Kd), N) == nb_of(kt_of(Kd2), N2);
 }
@@ -210,25 +220,32 @@ int launch_lin_decay_grad(const LinArgs &a, const float *dq_dot, int q_tiles, co
 
 // ---- gradients of shared q, k heads ----------------------------------------------------------------
 
+// dq (blockIdx.y 0) and dk (1)
 template <class Ty>
-__global__ __launch_bounds__(256) void k_lin_head_sum(size_t n, int r, int D, const float *in,
-                                                      typename Ty::T *out) {
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) {
-        const size_t row = i / D;
-        const float *p = in + row * r * D + i % D;
+__global__ __launch_bounds__(256) void k_lin_head_sum(size_t n, int r, uint32_t D, const float *dq, const float *dk,
+                                                      typename Ty::T *dq_out, typename Ty::T *dk_out) {
+    const float *in = blockIdx.y ? dk : dq;
+    typename Ty::T *out = blockIdx.y ? dk_out : dq_out;
+    for (size_t i0 = (size_t)blockIdx.x * 256; i0 < n; i0 += (size_t)gridDim.x * 256) {
+        if (i0 + threadIdx.x >= n) return;
+        // (one long division for all threads)
+        const size_t row0 = i0 / D;
+        const uint32_t d0 = (uint32_t)(i0 - row0 * D) + threadIdx.x, row = d0 / D, d = d0 % D;
+        const float *p = in + (row0 + row) * r * D + d;
         float s = 0.f;
         for (int j = 0; j < r; ++j) s += p[(size_t)j * D];
-        out[i] = Ty::down(s);
+        out[i0 + threadIdx.x] = Ty::down(s);
     }
 }
 
-int launch_lin_head_sum(int dtype, size_t rows, int Hk, int r, int D, const float *in, void *out, hipStream_t st) {
+int launch_lin_head_sum(int dtype, size_t rows, int Hk, int r, int D, const float *dq, const float *dk, void *dq_out,
+                        void *dk_out, hipStream_t st) {
     const size_t n = rows * Hk * D, blocks = (n + 255) / 256;
     return with_dtype(dtype, [&](auto ty) {
         using Ty = decltype(ty);
         KTimer kt("k_lin_head_sum", st);
-        hipLaunchKernelGGL(k_lin_head_sum<Ty>, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, st, n, r,
-                           D, in, (typename Ty::T *)out);
+        hipLaunchKernelGGL(k_lin_head_sum<Ty>, dim3((unsigned)(blocks < 65536 ? blocks : 65536), 2), dim3(256), 0, st, n, r,
+                           (uint32_t)D, dq, dk, (typename Ty::T *)dq_out, (typename Ty::T *)dk_out);
         DEER_LAUNCH_CHECK("k_lin_head_sum");
         return (int)DEER_OK;
     });

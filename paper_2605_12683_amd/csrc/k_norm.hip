@@ -211,10 +211,13 @@ __global__ __launch_bounds__(block_of(TEAM)) void k_layernorm_adj(NormArgs a, in
     }
 }
 
-// out[g, d] = sum over the partials of group g (g, g + G, ...): 32 columns by 8 slices a block, in
-// float64
-__global__ __launch_bounds__(256) void k_layernorm_sum(int G, int D, int np, const float *part, float *dw, float *db) {
-    __shared__ double sh[8][32];
+// out[g, d] = sum over the partials of group g (g, g + G, ...): 32 columns by SL slices a block, in
+// float64.  Each slice's chain of loads is what takes the time: 32 slices where a group has hundreds
+// of partials (515 columns of 701: 9.2 us with 8 slices, XXX with 32), 8 where it has few.
+template <int SL>
+__global__ __launch_bounds__(32 * SL) void k_layernorm_sum(int G, int D, int np, const float *part, float *dw,
+                                                           float *db) {
+    __shared__ double sh[SL][32];
     float *out = blockIdx.y ? db : dw;
     if (!out) return;
     const int per = (D + 31) / 32, grp = blockIdx.x / per, c = threadIdx.x & 31, sl = threadIdx.x >> 5;
@@ -224,12 +227,12 @@ __global__ __launch_bounds__(256) void k_layernorm_sum(int G, int D, int np, con
         const float *p = part + (size_t)blockIdx.y * D + d;
         const size_t step = (size_t)2 * D;
 #pragma unroll 8
-        for (int i = grp + G * sl; i < np; i += 8 * G) s += (double)p[i * step];
+        for (int i = grp + G * sl; i < np; i += SL * G) s += (double)p[i * step];
     }
     sh[sl][c] = s;
     __syncthreads();
     if (sl == 0 && d < D) {
-        for (int i = 1; i < 8; ++i) s += sh[i][c];
+        for (int i = 1; i < SL; ++i) s += sh[i][c];
         out[(size_t)grp * D + d] = (float)s;
     }
 }
@@ -394,8 +397,10 @@ size_t layernorm_adjoint_ws_bytes(const NormArgs &a) { return (size_t)partials_o
 
 static int launch_sum(const NormArgs &a, const float *part, float *dw, float *db, hipStream_t st) {
     KTimer kt("k_layernorm_sum", st);
-    hipLaunchKernelGGL(k_layernorm_sum, dim3((unsigned)(a.G * ((a.D + 31) / 32)), 2), dim3(256), 0, st, a.G, a.D,
-                       partials_of(a), part, dw, db);
+    const int np = partials_of(a);
+    const dim3 grid((unsigned)(a.G * ((a.D + 31) / 32)), 2);
+    if (np / a.G > 128) hipLaunchKernelGGL(k_layernorm_sum<32>, grid, dim3(1024), 0, st, a.G, a.D, np, part, dw, db);
+    else hipLaunchKernelGGL(k_layernorm_sum<8>, grid, dim3(256), 0, st, a.G, a.D, np, part, dw, db);
     DEER_LAUNCH_CHECK("k_layernorm_sum");
     return DEER_OK;
 }

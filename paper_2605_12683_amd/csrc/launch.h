@@ -365,6 +365,7 @@ struct LinArgs {
     bool joined;                // seg holds the state entering each segment, not what each adds
 };
 int lin_tiles(int Kd, int N);   // blocks that share the N columns of one head's state
+int lin_resident(int dtype, int Kd, int N, bool dots);   // a walk's blocks per CU
 bool lin_same_tile(int Kd, int N, int Kd2, int N2);
 // all roles of one call have the same tile shape; states: what each segment adds (into seg,
 // seg_decay), else the outputs; dots: and dot, anchor (which are summed over many steps, so the
@@ -380,8 +381,9 @@ int launch_lin_walk_f32(const LinArgs &a, const LinRole *roles, int n, bool stat
 int launch_lin_decay_grad(const LinArgs &a, const float *dq_dot, int q_tiles, const float *dk_dot, int k_tiles,
                           const float *fwd_anchor, const float *rev_anchor, int elems, double *part, float *dlog_decay,
                           hipStream_t st);
-// out[b, t, hk, :] = sum over the r heads that share hk of in[b, t, hk r + i, :]
-int launch_lin_head_sum(int dtype, size_t rows, int Hk, int r, int D, const float *in, void *out, hipStream_t st);
+// dq_out[b, t, hk, :] = sum over the r heads that share hk of dq[b, t, hk r + i, :]; dk_out likewise
+int launch_lin_head_sum(int dtype, size_t rows, int Hk, int r, int D, const float *dq, const float *dk, void *dq_out,
+                        void *dk_out, hipStream_t st);
 struct LinStep {
     int dtype, B, H, Hk, Dk, Dv;
     bool per_seq;               // log_decay [B, H] instead of [H]

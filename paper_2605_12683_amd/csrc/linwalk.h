@@ -107,6 +107,27 @@ struct LinRoles {
     LinRole r[3];
 };
 
+template <int KT_, int NW_, int CT_>
+struct WalkShape {
+    static constexpr int KT = KT_, NW = NW_, CT = CT_;
+};
+
+// f(WalkShape) of operands of NPI parts
+template <int NPI, class Fn>
+int with_walk_shape(int Kd, int N, Fn f) {
+    const int KT = kt_of(Kd);
+    if (KT == 256) return f(WalkShape<256, 4, 1>{});
+    if (nb_of(KT, N) == 64) {
+        if (KT == 32) return f(WalkShape<32, 4, 1>{});
+        if (KT == 64) return f(WalkShape<64, 4, 1>{});
+        return f(WalkShape<128, 4, 1>{});
+    }
+    constexpr int NW = NPI == 3 ? 8 : 4, CT = 8 / NW;
+    if (KT == 32) return f(WalkShape<32, NW, CT>{});
+    if (KT == 64) return f(WalkShape<64, NW, CT>{});
+    return f(WalkShape<128, NW, CT>{});
+}
+
 // ---- loads of a chunk's rows -----------------------------------------------------------------
 
 typedef uint32_t v2u __attribute__((ext_vector_type(2)));
@@ -880,18 +901,9 @@ int launch_walk_tile(const LinArgs &a, const LinRole *roles, int n, hipStream_t 
 
 template <class Ty, int NPX, int MODE>
 int launch_walk_parts(const LinArgs &a, const LinRole *roles, int n, hipStream_t st) {
-    constexpr int NPI = InParts<Ty>::n;
-    const int KT = kt_of(roles[0].Kd), nb = nb_of(KT, roles[0].N);
-    if (KT == 256) return launch_walk_tile<Ty, 256, 4, 1, NPX, MODE>(a, roles, n, st);
-    if (nb == 64) {
-        if (KT == 32) return launch_walk_tile<Ty, 32, 4, 1, NPX, MODE>(a, roles, n, st);
-        if (KT == 64) return launch_walk_tile<Ty, 64, 4, 1, NPX, MODE>(a, roles, n, st);
-        return launch_walk_tile<Ty, 128, 4, 1, NPX, MODE>(a, roles, n, st);
-    }
-    constexpr int NW = NPI == 3 ? 8 : 4, CT = 8 / NW;
-    if (KT == 32) return launch_walk_tile<Ty, 32, NW, CT, NPX, MODE>(a, roles, n, st);
-    if (KT == 64) return launch_walk_tile<Ty, 64, NW, CT, NPX, MODE>(a, roles, n, st);
-    return launch_walk_tile<Ty, 128, NW, CT, NPX, MODE>(a, roles, n, st);
+    return with_walk_shape<InParts<Ty>::n>(roles[0].Kd, roles[0].N, [&](auto s) {
+        return launch_walk_tile<Ty, s.KT, s.NW, s.CT, NPX, MODE>(a, roles, n, st);
+    });
 }
 
 }  // namespace deer
