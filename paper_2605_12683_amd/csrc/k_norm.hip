@@ -125,8 +125,9 @@ __global__ __launch_bounds__(block_of(TEAM)) void k_layernorm_adj(NormArgs a, in
     const int lane = threadIdx.x % TEAM, in_block = threadIdx.x / TEAM, team = blockIdx.x * TPB + in_block;
     const T *x = (const T *)a.x;
     const bool on = team < nt;
-    // 1024 threads have 128 registers each: no room for the next row beside this one
-    constexpr bool AHEAD = TEAM < 1024;
+    // of the next row, x and g are loaded while this one is reduced, or where registers are few only x, or
+    // none (1024 threads, 128 registers each)
+    constexpr bool BOTH = TEAM * NV < 2048, AHEAD = TEAM < 1024;
     float dw[NV][E], db[NV][E];
 #pragma unroll
     for (int v = 0; v < NV; ++v)
@@ -136,19 +137,22 @@ __global__ __launch_bounds__(block_of(TEAM)) void k_layernorm_adj(NormArgs a, in
         float w[NV][E];
         v4u nx[NV], ng[NV];
         float nm, nr;
-        auto load = [&](size_t row) {
+        auto load_x = [&](size_t row) {
 #pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                nx[v] = load_unit<Ty>(x + row * a.D, (v * TEAM + lane) * E, a.D, vec);
-                ng[v] = load_unit<Ty>(g + row * a.D, (v * TEAM + lane) * E, a.D, vec);
-            }
+            for (int v = 0; v < NV; ++v) nx[v] = load_unit<Ty>(x + row * a.D, (v * TEAM + lane) * E, a.D, vec);
             nm = mean[row], nr = rstd[row];
         };
-        if (AHEAD) load(team);
+        auto load_g = [&](size_t row) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v) ng[v] = load_unit<Ty>(g + row * a.D, (v * TEAM + lane) * E, a.D, vec);
+        };
+        if (AHEAD) load_x(team);
+        if (BOTH) load_g(team);
         load_weights<E, NV, TEAM>(a, a.w, team % a.G, lane, 1.f, w);
         const float width = (float)a.D;   // divided by: the mean of equal numbers is that number
         for (size_t row = team; row < a.rows; row += nt) {
-            if (!AHEAD) load(row);
+            if (!AHEAD) load_x(row);
+            if (!BOTH) load_g(row);
             const float m = nm, r = nr;
             float xh[NV][E], u[NV][E], s1 = 0.f, s2 = 0.f;
 #pragma unroll
@@ -165,7 +169,10 @@ __global__ __launch_bounds__(block_of(TEAM)) void k_layernorm_adj(NormArgs a, in
                     s2 = fmaf(u[v][e], xh[v][e], s2);
                 }
             }
-            if (AHEAD && row + nt < a.rows) load(row + nt);
+            if (AHEAD && row + nt < a.rows) {
+                load_x(row + nt);
+                if (BOTH) load_g(row + nt);
+            }
             if (!dx) continue;
             s1 = sum(s1) / width;
             s2 = sum(s2) / width;
@@ -213,7 +220,7 @@ __global__ __launch_bounds__(block_of(TEAM)) void k_layernorm_adj(NormArgs a, in
 
 // out[g, d] = sum over the partials of group g (g, g + G, ...): 32 columns by SL slices a block, in
 // float64.  Each slice's chain of loads is what takes the time: 32 slices where a group has hundreds
-// of partials (515 columns of 701: 9.2 us with 8 slices, XXX with 32), 8 where it has few.
+// of partials (515 columns of 701: 9.2 us with 8 slices, 6.1 with 32), 8 where it has few.
 template <int SL>
 __global__ __launch_bounds__(32 * SL) void k_layernorm_sum(int G, int D, int np, const float *part, float *dw,
                                                            float *db) {
@@ -314,12 +321,14 @@ __global__ __launch_bounds__(256) void k_layernorm_long_part(NormArgs a, const t
 // ---- launches -------------------------------------------------------------------------------------
 
 // threads per row and units per thread: two units where a row has them, so that enough is in flight
-// (rows of 2048 in bf16: 53 us with 128 threads, 62 us with 256 of one unit); at most 16 elements a
-// thread, of which the adjoint holds six float32 values each; 0: none holds the row
+// (rows of 2048 in bf16: 53 us with 128 threads, 62 us with 256 of one unit).  1024 threads have 128
+// registers each, which hold 16 elements a thread, but for the adjoint, with six float32 values for
+// each, not the next row as well: it takes 512 threads where these can hold the row (4096 rows of
+// 16384 in bf16: 105 us for 144; forwards 65 for 59).  0: none holds the row
 struct NormShape {
     int team, nv;
 };
-static NormShape shape_of(int dtype, int D) {
+static NormShape shape_of(int dtype, int D, bool adjoint) {
     const int e = dtype == DEER_F32 ? 4 : 8, u = (D + e - 1) / e;
     if (u <= 16) return {16, 1};
     if (u <= 64) return {64, 1};
@@ -327,7 +336,7 @@ static NormShape shape_of(int dtype, int D) {
     if (u <= 256) return {128, 2};
     if (u <= 512) return {256, 2};
     if (u <= 1024) return {512, 2};
-    if (u <= 2048) return {1024, 2};
+    if (u <= 2048) return adjoint ? NormShape{512, 4} : NormShape{1024, 2};
     if (u <= 4096 && dtype == DEER_F32) return {1024, 4};
     return {0, 0};
 }
@@ -341,7 +350,7 @@ static int teams_of(size_t rows, int G, int team, size_t threads) {
 constexpr size_t kForwardThreads = 256 * 1024, kAdjointThreads = 256 * 512;
 
 static int partials_of(const NormArgs &a) {
-    const NormShape s = shape_of(a.dtype, a.D);
+    const NormShape s = shape_of(a.dtype, a.D, true);
     if (!s.team) return kLongSplits * a.G;
     const int nt = teams_of(a.rows, a.G, s.team, kAdjointThreads), tpb = block_of(s.team) / s.team;
     return a.G > 1 ? nt : (nt + tpb - 1) / tpb;
@@ -350,18 +359,19 @@ static int partials_of(const NormArgs &a) {
 template <int N>
 using Int = std::integral_constant<int, N>;
 
-template <class Fn>
+template <bool ADJOINT, class Fn>
 static int with_shape(const NormArgs &a, Fn f) {
-    const NormShape s = shape_of(a.dtype, a.D);
+    const NormShape s = shape_of(a.dtype, a.D, ADJOINT);
     return with_dtype(a.dtype, [&](auto ty) {
         if (s.team == 16) return f(ty, Int<16>{}, Int<1>{});
         if (s.team == 64) return s.nv == 1 ? f(ty, Int<64>{}, Int<1>{}) : f(ty, Int<64>{}, Int<2>{});
         if (s.team == 128) return f(ty, Int<128>{}, Int<2>{});
         if (s.team == 256) return f(ty, Int<256>{}, Int<2>{});
-        if (s.team == 512) return f(ty, Int<512>{}, Int<2>{});
+        if (s.team == 512 && s.nv == 2) return f(ty, Int<512>{}, Int<2>{});
         if constexpr (std::is_same<decltype(ty), F32>::value)
-            if (s.nv == 4) return f(ty, Int<1024>{}, Int<4>{});
-        return f(ty, Int<1024>{}, Int<2>{});
+            if (s.nv == 4 && s.team == 1024) return f(ty, Int<1024>{}, Int<4>{});
+        if constexpr (ADJOINT) return f(ty, Int<512>{}, Int<4>{});
+        else return f(ty, Int<1024>{}, Int<2>{});
     });
 }
 
@@ -372,7 +382,7 @@ static bool units_whole(const NormArgs &a, const void *p, const void *q) {
 }
 
 int launch_layernorm(const NormArgs &a, void *y, float *mean, float *rstd, hipStream_t st) {
-    const NormShape s = shape_of(a.dtype, a.D);
+    const NormShape s = shape_of(a.dtype, a.D, false);
     KTimer kt("k_layernorm", st);
     if (!s.team)
         return with_dtype(a.dtype, [&](auto ty) {
@@ -383,7 +393,7 @@ int launch_layernorm(const NormArgs &a, void *y, float *mean, float *rstd, hipSt
             return (int)DEER_OK;
         });
     const int nt = teams_of(a.rows, a.G, s.team, kForwardThreads);
-    return with_shape(a, [&](auto ty, auto team, auto nv) {
+    return with_shape<false>(a, [&](auto ty, auto team, auto nv) {
         using Ty = decltype(ty);
         constexpr int TEAM = decltype(team)::value, NV = decltype(nv)::value, TPB = block_of(TEAM) / TEAM;
         hipLaunchKernelGGL((k_layernorm<Ty, TEAM, NV>), dim3((nt + TPB - 1) / TPB), dim3(block_of(TEAM)), 0, st, a, nt,
@@ -407,7 +417,7 @@ static int launch_sum(const NormArgs &a, const float *part, float *dw, float *db
 
 int launch_layernorm_adjoint(const NormArgs &a, const void *g, const float *mean, const float *rstd, void *dx,
                              float *dw, float *db, void *ws, hipStream_t st) {
-    const NormShape s = shape_of(a.dtype, a.D);
+    const NormShape s = shape_of(a.dtype, a.D, true);
     const bool sums = dw || db;
     float *part = sums ? (float *)ws : nullptr;
     int rc;
@@ -430,7 +440,7 @@ int launch_layernorm_adjoint(const NormArgs &a, const void *g, const float *mean
         });
     } else {
         const int nt = teams_of(a.rows, a.G, s.team, kAdjointThreads);
-        rc = with_shape(a, [&](auto ty, auto team, auto nv) {
+        rc = with_shape<true>(a, [&](auto ty, auto team, auto nv) {
             using Ty = decltype(ty);
             using T = typename Ty::T;
             constexpr int TEAM = decltype(team)::value, NV = decltype(nv)::value, TPB = block_of(TEAM) / TEAM;
