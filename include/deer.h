@@ -405,7 +405,7 @@ int deer_linattn_step(const deer_linattn_shape *shape, int B, const deer_view *q
 typedef struct {
     int dtype;          /* DEER_F32, DEER_BF16 or DEER_F16: x, y, g, dx                        */
     int wtype;          /* of w and b: DEER_F32 or dtype                                      */
-    int G, D;           /* D in 1..65536                                                      */
+    int G, D;           /* D in 1..65536, G in 1..2^20, G D at most 2^24                       */
     const void *w;      /* [G, D] or NULL (ones)                                              */
     const void *b;      /* [G, D] or NULL (zeros)                                             */
     float eps;          /* >= 0                                                               */

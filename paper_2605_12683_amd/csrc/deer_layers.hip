@@ -146,7 +146,10 @@ static int check_norm(const deer_norm *n, int64_t rows) {
         set_error("rows must be a positive multiple of G (rows=%lld, G=%d)", (long long)rows, n->G);
         return DEER_ERR_INVALID_ARG;
     }
-    if ((long)n->G * n->D > (1L << 24)) { set_error("G D must not exceed 2^24 (G=%d, D=%d)", n->G, n->D); return DEER_ERR_INVALID_ARG; }
+    if (n->G > (1 << 20) || (long)n->G * n->D > (1L << 24)) {
+        set_error("G must not exceed 2^20, nor G D 2^24 (G=%d, D=%d)", n->G, n->D);
+        return DEER_ERR_INVALID_ARG;
+    }
     if (!(n->eps >= 0.f) || !isfinite(n->eps)) { set_error("eps must be finite and not negative"); return DEER_ERR_INVALID_ARG; }
     return DEER_OK;
 }

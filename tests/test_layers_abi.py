@@ -127,7 +127,7 @@ def _norm(**kw):
 @pytest.mark.parametrize("kw,rows", [
     (dict(dtype=9), 4), (dict(wtype=_b.DEER_F16), 4), (dict(wtype=7), 4), (dict(G=0), 4), (dict(D=0), 4),
     (dict(D=65537), 4), (dict(G=1 << 12, D=1 << 13), 1 << 12), (dict(eps=-1e-9), 4), (dict(eps=float("nan")), 4),
-    (dict(eps=float("inf")), 4), (dict(), 0), (dict(), -2), (dict(), 3)])
+    (dict(eps=float("inf")), 4), (dict(G=(1 << 20) + 1, D=1), (1 << 20) + 1), (dict(), 0), (dict(), -2), (dict(), 3)])
 def test_norms(lib, kw, rows):
     n = _norm(**kw)
     assert lib.deer_layernorm_workspace_bytes(n, rows) == 0
