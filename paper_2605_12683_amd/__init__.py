@@ -16,7 +16,6 @@ the current stream of the tensors' GPU.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import threading
 
@@ -456,7 +455,8 @@ def _operand(name, t, gpu=None, shape=None, dtype=None):
     return t
 
 
-# the current stream of a GPU as an integer; torch's own call builds a Stream object first
+# the current GPU, and the current stream of a GPU as an integer; torch's public calls build objects first
+_current_gpu = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
     (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
@@ -465,29 +465,36 @@ def _at(t):
     return None if t is None else t.data_ptr()
 
 
-_already = contextlib.nullcontext()
+def _run(gpu, where, *args):
+    """Calls the layer `where` of the library with the current stream of a GPU, which is the current one meanwhile."""
+    call = getattr(_b._lib, where)
+    if _current_gpu() == gpu:
+        st = call(*args, _raw_stream(gpu))
+    else:
+        with torch.cuda.device(gpu):
+            st = call(*args, _raw_stream(gpu))
+    if st:
+        _b._check(st, where)
 
 
-def _on(gpu):
-    """Makes a GPU the current one (nothing to do if it is)."""
-    return _already if torch.cuda.current_device() == gpu else torch.cuda.device(gpu)
+def _like(t):
+    """A new contiguous tensor of t's shape and type on its GPU."""
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
 def _result(name, t, gpu, shape, dtype):
-    """A caller's output buffer, or a new one on the current GPU, which is that of index gpu."""
-    if t is None:
-        return torch.empty(shape, dtype=dtype, device="cuda")
+    """A caller's output buffer."""
     if not _operand(name, t, gpu, shape, dtype).is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t
 
 
-def _scratch(ws, gpu, need):
-    """A caller's workspace, or a new one, and its size in bytes."""
+def _scratch(ws, like, need):
+    """A caller's workspace, or a new one on the GPU of another tensor, and its size in bytes."""
     if ws is None:
-        ws = torch.empty(need or 256, dtype=torch.uint8, device="cuda")
+        ws = like.new_empty(need or 256, dtype=torch.uint8)
         return ws, ws.numel()
-    if not _operand("ws", ws, gpu).is_contiguous():
+    if not _operand("ws", ws, like.get_device()).is_contiguous():
         raise ValueError("ws must be contiguous")
     return ws, ws.numel() * ws.element_size()
 
@@ -506,26 +513,27 @@ class _Lin:
     def __init__(self, dim, q, k, v, log_decay, scale, lengths):
         if _operand("v", v).dim() != dim:
             raise ValueError("v must be [B, T, H, Dv]" if dim == 4 else "v must be [B, H, Dv]")
-        dtype, gpu = v.dtype, v.get_device()
+        dtype, gpu, shape = v.dtype, v.get_device(), v.shape
         if dtype not in _DTYPES:
             raise ValueError(f"unsupported type {dtype}")
-        *lead, H, Dv = v.shape
-        if max(v.shape) >> 31:
-            raise ValueError(f"a dimension of 2^31 or more: {tuple(v.shape)}")
-        _operand("k", k, gpu, None, dtype)
-        if _operand("q", q, gpu, k.shape, dtype).dim() != dim or list(q.shape[:-2]) != lead:
-            raise ValueError(f"q must be {lead} by heads by Dk, not {tuple(q.shape)}")
-        Hk, Dk = q.shape[-2:]
-        if max(Hk, Dk) >> 31:
-            raise ValueError(f"a dimension of 2^31 or more: {tuple(q.shape)}")
-        per_step = _operand("log_decay", log_decay, gpu, None, torch.float32).dim() > 1
-        _operand("log_decay", log_decay, gpu, (*lead, H) if per_step else (H,))
+        qk = _operand("q", q, gpu, None, dtype).shape
+        _operand("k", k, gpu, qk, dtype)
+        if len(qk) != dim or qk[:-2] != shape[:-2]:
+            raise ValueError(f"q must be {list(shape[:-2])} by heads by Dk, not {tuple(qk)}")
+        if (v.numel() >> 31 and max(shape) >> 31) or (q.numel() >> 31 and max(qk) >> 31):
+            raise ValueError(f"a dimension of 2^31 or more: {tuple(shape)}, {tuple(qk)}")
+        decays = _operand("log_decay", log_decay, gpu, None, torch.float32).shape
+        per_step = len(decays) > 1
+        if decays != (shape[:-1] if per_step else shape[-2:-1]):
+            raise ValueError(f"log_decay must have the shape {tuple(shape[-2:-1])} or {tuple(shape[:-1])}, "
+                             f"not {tuple(decays)}")
+        B, H = shape[0], shape[-2]
         if lengths is not None:
-            lengths = _operand("lengths", lengths, gpu, (lead[0],), torch.int32).contiguous()
-        self.gpu, self.B, self.T, self.shape = gpu, lead[0], lead[1] if dim == 4 else 1, (lead[0], H, Dk, Dv)
+            lengths = _operand("lengths", lengths, gpu, (B,), torch.int32).contiguous()
+        self.gpu, self.B, self.T, self.shape = gpu, B, shape[1] if dim == 4 else 1, (B, H, qk[-1], shape[-1])
         (self.q, self.vq), (self.k, self.vk), (self.v, self.vv) = _view(q), _view(k), _view(v)
         self.log_decay, self.lengths = log_decay.contiguous(), lengths
-        self.c = _b.deer_linattn_shape(_DTYPES[dtype], H, Hk, Dk, Dv, per_step, float(scale))
+        self.c = _b.deer_linattn_shape(_DTYPES[dtype], H, qk[-2], qk[-1], shape[-1], per_step, float(scale))
 
     def matrix(self, name, t):
         """A state or its cotangent, contiguous."""
@@ -535,7 +543,7 @@ class _Lin:
 
     def scratch(self, lib, ws, op):
         need = 0 if ws is not None else lib.deer_linattn_workspace_bytes(ctypes.byref(self.c), self.B, self.T, op)
-        return _scratch(ws, self.gpu, need)
+        return _scratch(ws, self.v, need)
 
 
 def deer_linattn_workspace_bytes(B: int, T: int, H: int, Hk: int, Dk: int, Dv: int, op: int,
@@ -558,16 +566,15 @@ def deer_linattn(q, k, v, log_decay, *, scale: float = 1.0, lengths=None, state0
     Returns dict(o [B, T, H, Dv], state (None unless want_state or a buffer is given))."""
     lib = load()
     a = _Lin(4, q, k, v, log_decay, scale, lengths)
-    with _on(a.gpu):
-        o = _result("o", o, a.gpu, v.shape, v.dtype)
-        s0 = a.matrix("state0", state0)
-        if state is not None or want_state:
-            state = _result("state", state, a.gpu, a.shape, torch.float32)
-        ws, ws_bytes = a.scratch(lib, ws, _b.DEER_OP_SOLVE)
-        st = lib.deer_linattn(ctypes.byref(a.c), a.B, a.T, ctypes.byref(a.vq), ctypes.byref(a.vk), ctypes.byref(a.vv),
-                              _at(a.log_decay), _at(a.lengths), _at(s0), _at(o), _at(state), _at(ws), ws_bytes,
-                              _raw_stream(a.gpu))
-    _b._check(st, "deer_linattn")
+    o = _like(v) if o is None else _result("o", o, a.gpu, v.shape, v.dtype)
+    s0 = a.matrix("state0", state0)
+    if state is not None:
+        _result("state", state, a.gpu, a.shape, torch.float32)
+    elif want_state:
+        state = v.new_empty(a.shape, dtype=torch.float32)
+    ws, ws_bytes = a.scratch(lib, ws, _b.DEER_OP_SOLVE)
+    _run(a.gpu, "deer_linattn", ctypes.byref(a.c), a.B, a.T, ctypes.byref(a.vq), ctypes.byref(a.vk), ctypes.byref(a.vv),
+         _at(a.log_decay), _at(a.lengths), _at(s0), _at(o), _at(state), _at(ws), ws_bytes)
     return {"o": o, "state": state}
 
 
@@ -578,21 +585,17 @@ def deer_linattn_adjoint(q, k, v, log_decay, g, *, scale: float = 1.0, lengths=N
     state0 (if state0 is given)}); q, k, v in the operands' type, the others in float32."""
     lib = load()
     a = _Lin(4, q, k, v, log_decay, scale, lengths)
-    with _on(a.gpu):
-        gt, vg = _view(_operand("g", g, a.gpu, v.shape, v.dtype))
-        s0, gs = a.matrix("state0", state0), a.matrix("g_state", g_state)
-        grads = {n: torch.empty(x.shape, dtype=x.dtype, device="cuda") for n, x in (("q", q), ("k", k), ("v", v))}
-        if want_decay:
-            grads["log_decay"] = torch.empty(log_decay.shape, dtype=torch.float32, device="cuda")
-        if s0 is not None:
-            grads["state0"] = torch.empty(a.shape, dtype=torch.float32, device="cuda")
-        ws, ws_bytes = a.scratch(lib, ws, _b.DEER_OP_ADJOINT)
-        st = lib.deer_linattn_adjoint(ctypes.byref(a.c), a.B, a.T, ctypes.byref(a.vq), ctypes.byref(a.vk),
-                                      ctypes.byref(a.vv), _at(a.log_decay), _at(a.lengths), _at(s0),
-                                      ctypes.byref(vg), _at(gs), _at(grads["q"]), _at(grads["k"]), _at(grads["v"]),
-                                      _at(grads.get("log_decay")), _at(grads.get("state0")), _at(ws), ws_bytes,
-                                      _raw_stream(a.gpu))
-    _b._check(st, "deer_linattn_adjoint")
+    gt, vg = _view(_operand("g", g, a.gpu, v.shape, v.dtype))
+    s0, gs = a.matrix("state0", state0), a.matrix("g_state", g_state)
+    grads = {"q": _like(q), "k": _like(k), "v": _like(v)}
+    if want_decay:
+        grads["log_decay"] = _like(log_decay)
+    if s0 is not None:
+        grads["state0"] = _like(s0)
+    ws, ws_bytes = a.scratch(lib, ws, _b.DEER_OP_ADJOINT)
+    _run(a.gpu, "deer_linattn_adjoint", ctypes.byref(a.c), a.B, a.T, ctypes.byref(a.vq), ctypes.byref(a.vk),
+         ctypes.byref(a.vv), _at(a.log_decay), _at(a.lengths), _at(s0), ctypes.byref(vg), _at(gs), _at(grads["q"]),
+         _at(grads["k"]), _at(grads["v"]), _at(grads.get("log_decay")), _at(grads.get("state0")), _at(ws), ws_bytes)
     return {"grads": grads}
 
 
@@ -600,14 +603,12 @@ def deer_linattn_step(q, k, v, log_decay, state, *, scale: float = 1.0, lengths=
     """One step of deer_linattn for every sequence (generation): q, k [B, Hk, Dk], v [B, H, Dv],
     log_decay [H] or [B, H]; state float32 [B, H, Dk, Dv], contiguous, is updated in place.  A sequence
     whose entry of lengths (int32 [B]) is 0 takes no step.  Returns dict(o [B, H, Dv], state)."""
-    lib = load()
+    load()
     a = _Lin(3, q, k, v, log_decay, scale, lengths)
-    with _on(a.gpu):
-        state = _result("state", _operand("state", state), a.gpu, a.shape, torch.float32)
-        o = _result("o", o, a.gpu, v.shape, v.dtype)
-        st = lib.deer_linattn_step(ctypes.byref(a.c), a.B, ctypes.byref(a.vq), ctypes.byref(a.vk), ctypes.byref(a.vv),
-                                   _at(a.log_decay), _at(a.lengths), _at(state), _at(o), _raw_stream(a.gpu))
-    _b._check(st, "deer_linattn_step")
+    _result("state", state, a.gpu, a.shape, torch.float32)
+    o = _like(v) if o is None else _result("o", o, a.gpu, v.shape, v.dtype)
+    _run(a.gpu, "deer_linattn_step", ctypes.byref(a.c), a.B, ctypes.byref(a.vq), ctypes.byref(a.vk), ctypes.byref(a.vv),
+         _at(a.log_decay), _at(a.lengths), _at(state), _at(o))
     return {"o": o, "state": state}
 
 
@@ -648,14 +649,12 @@ def deer_layernorm(x, w=None, b=None, *, eps: float = 1e-5, y=None) -> dict:
     """Layer normalisation over the last dimension of x (float32, bfloat16 or float16):
     y = (x - mean) rstd w + b.  w, b: [D], or [G, D] with x [..., G, D] (weights of its own for each
     head), float32 or x's type, or None.  Returns dict(y, mean, rstd), the statistics in float32."""
-    lib = load()
+    load()
     gpu, xc, wc, bc, rows, c = _norm(x, w, b, eps)
-    with _on(gpu):
-        y = _result("y", y, gpu, x.shape, x.dtype)
-        mean = torch.empty(x.shape[:-1], dtype=torch.float32, device="cuda")
-        rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device="cuda")
-        st = lib.deer_layernorm(ctypes.byref(c), rows, _at(xc), _at(y), _at(mean), _at(rstd), _raw_stream(gpu))
-    _b._check(st, "deer_layernorm")
+    y = _like(x) if y is None else _result("y", y, gpu, x.shape, x.dtype)
+    mean = x.new_empty(x.shape[:-1], dtype=torch.float32)
+    rstd = torch.empty_like(mean)
+    _run(gpu, "deer_layernorm", ctypes.byref(c), rows, _at(xc), _at(y), _at(mean), _at(rstd))
     return {"y": y, "mean": mean, "rstd": rstd}
 
 
@@ -664,17 +663,14 @@ def deer_layernorm_adjoint(x, g, mean, rstd, w=None, *, want_grads: bool = True,
     dL/dx in x's type, grads = {w, b} in float32, of w's shape ([D] without w); {} without want_grads)."""
     lib = load()
     gpu, xc, wc, _, rows, c = _norm(x, w, None, 0.0)
-    with _on(gpu):
-        gc = _operand("g", g, gpu, x.shape, x.dtype).contiguous()
-        mc = _operand("mean", mean, gpu, x.shape[:-1], torch.float32).contiguous()
-        rc = _operand("rstd", rstd, gpu, x.shape[:-1], torch.float32).contiguous()
-        dx = torch.empty(x.shape, dtype=x.dtype, device="cuda")
-        grads = {}
-        if want_grads:
-            shape = x.shape[-1:] if w is None else w.shape
-            grads = {n: torch.empty(shape, dtype=torch.float32, device="cuda") for n in ("w", "b")}
-        ws, ws_bytes = _scratch(ws, gpu, 0 if ws is not None else lib.deer_layernorm_workspace_bytes(ctypes.byref(c), rows))
-        st = lib.deer_layernorm_adjoint(ctypes.byref(c), rows, _at(xc), _at(gc), _at(mc), _at(rc), _at(dx),
-                                        _at(grads.get("w")), _at(grads.get("b")), _at(ws), ws_bytes, _raw_stream(gpu))
-    _b._check(st, "deer_layernorm_adjoint")
+    gc = _operand("g", g, gpu, x.shape, x.dtype).contiguous()
+    mc = _operand("mean", mean, gpu, x.shape[:-1], torch.float32).contiguous()
+    rc = _operand("rstd", rstd, gpu, x.shape[:-1], torch.float32).contiguous()
+    dx, grads = _like(x), {}
+    if want_grads:
+        dw = x.new_empty(x.shape[-1:] if w is None else w.shape, dtype=torch.float32)
+        grads = {"w": dw, "b": torch.empty_like(dw)}
+    ws, ws_bytes = _scratch(ws, x, 0 if ws is not None else lib.deer_layernorm_workspace_bytes(ctypes.byref(c), rows))
+    _run(gpu, "deer_layernorm_adjoint", ctypes.byref(c), rows, _at(xc), _at(gc), _at(mc), _at(rc), _at(dx),
+         _at(grads.get("w")), _at(grads.get("b")), _at(ws), ws_bytes)
     return {"x": dx, "grads": grads}
