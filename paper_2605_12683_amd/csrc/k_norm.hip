@@ -15,6 +15,23 @@
 
 namespace deer {
 
+// v plus that of the lane whose number differs in the bit OFF alone, with no trip through LDS.  Within
+// 16 lanes by rotation: lanes 8 apart are the same both ways, and of numbers that repeat every
+// 2 OFF lanes those OFF apart are.
+template <int OFF>
+__device__ __forceinline__ float add_across(float v) {
+    const uint32_t u = __float_as_uint(v);
+    if constexpr (OFF == 32) {
+        const auto p = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+        return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    } else if constexpr (OFF == 16) {
+        const auto p = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+        return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    } else {
+        return v + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)u, 0x120 + OFF, 15, 15, false));   // row_ror
+    }
+}
+
 // sum over a team; all its threads get it, the terms are always added in the same order
 template <int TEAM>
 struct TeamSum {
@@ -22,8 +39,8 @@ struct TeamSum {
     int flip = 0;
 
     __device__ __forceinline__ float operator()(float v) {
-#pragma unroll
-        for (int off = TEAM < 64 ? TEAM / 2 : 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+        if constexpr (TEAM >= 64) v = add_across<16>(add_across<32>(v));
+        v = add_across<1>(add_across<2>(add_across<4>(add_across<8>(v))));
         if constexpr (TEAM > 64) {
             constexpr int W = TEAM / 64;
             float *s = sh + flip * W;   // two buffers: one barrier a sum
