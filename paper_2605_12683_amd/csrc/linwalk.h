@@ -25,9 +25,14 @@
 //
 // What bounds it: a chunk of 64 steps at Kd = N = 128 in bf16 moves 64 KiB and takes 194 matrix
 // instructions of 16 x 16 x 32 a wave (1.5 us at their rate, against 3.3 us for the bytes at 5 TB/s
-// with all 256 CUs walking), so memory, as long as latencies are hidden: the next chunk's rows are
-// loaded into registers while this one is computed (barriers order LDS only), and tiles are kept
-// below 80 KiB of LDS, C = 32 instead of 64 where needed, so that two blocks share a CU.
+// with all 256 CUs walking).  Between them stand the vector instructions that split and scale what is
+// formed in between: of the issue cycles, vector and matrix instructions fill 58 + 25% (32 heads of
+// 64 x 64, 65536 steps, 768 blocks: 234 us, 2.9 TB/s) or 51 + 33% (dq and dk of 64 heads of 128 x
+// 128, 4096 steps, with dots: 188 us), and LDS is busy for 40%.  So the next chunk's rows are loaded
+// into registers while this one is computed (barriers order LDS only), the operands of the next
+// products are read from LDS while these run, what depends on the thread alone is not computed again
+// for every row, and tiles are kept below 80 KiB of LDS, C = 32 instead of 64 where needed, so that
+// two blocks share a CU.
 #pragma once
 
 #include <type_traits>
@@ -89,7 +94,9 @@ struct LinTile {
     static constexpr bool OUT = MODE != kStates;
     static constexpr int NB = 16 * NW * CT, TH = 64 * NW;
     // LDS row pitches, in which neither rows read 8 or 4 elements a lane nor rows read across meet in
-    // a bank (for 4 elements a lane: with k's columns of each 16 swapped by halves in rows 8..15 of 16)
+    // a bank (for 4 elements a lane: with k's columns of each 16 swapped by halves in rows 8..15 of 16);
+    // with KT + 8 for q, k as it is, and the scores' tiles stored apart, 38% of the LDS cycles were
+    // conflicts (32 heads of 64 x 64, 65536 steps: 265 us, 246 without)
     static constexpr int PQ = KT + 16, PK = KT + 16, PV = NB + 16;
     static constexpr int pairs(int C) { return C == 64 ? 6 : 2; }   // (16 outputs, 32 sources) not all above the diagonal
     static constexpr int bytes(int C) {
@@ -112,12 +119,12 @@ struct WalkShape {
     static constexpr int KT = KT_, NW = NW_, CT = CT_;
 };
 
-// f(WalkShape) of operands of NPI parts
+// f(WalkShape) of operands of NPI parts; narrow: 64 columns a block however many there are
 template <int NPI, class Fn>
-int with_walk_shape(int Kd, int N, Fn f) {
+int with_walk_shape(int Kd, int N, bool narrow, Fn f) {
     const int KT = kt_of(Kd);
     if (KT == 256) return f(WalkShape<256, 4, 1>{});
-    if (nb_of(KT, N) == 64) {
+    if (narrow || nb_of(KT, N) == 64) {
         if (KT == 32) return f(WalkShape<32, 4, 1>{});
         if (KT == 64) return f(WalkShape<64, 4, 1>{});
         return f(WalkShape<128, 4, 1>{});
@@ -901,7 +908,13 @@ int launch_walk_tile(const LinArgs &a, const LinRole *roles, int n, hipStream_t 
 
 template <class Ty, int NPX, int MODE>
 int launch_walk_parts(const LinArgs &a, const LinRole *roles, int n, hipStream_t st) {
-    return with_walk_shape<InParts<Ty>::n>(roles[0].Kd, roles[0].N, [&](auto s) {
+    // Where blocks of 128 columns leave half of the CUs without one, twice as many of 64, which take less
+    // time for a chunk (1 x 2048 steps, 4 heads of 128 x 128 in bf16: 33 us, narrow 27; with up to 256
+    // blocks the second reading of q and k costs more: 64 heads' adjoint 382, narrow 397).  Not with dots,
+    // which are laid out by blocks of 128.
+    const int nb = nb_of(kt_of(roles[0].Kd), roles[0].N), tiles = (roles[0].N + nb - 1) / nb;
+    const bool narrow = MODE != kOutDots && nb == 128 && (long)a.B * a.H * a.nseg * tiles * n <= 128;
+    return with_walk_shape<InParts<Ty>::n>(roles[0].Kd, roles[0].N, narrow, [&](auto s) {
         return launch_walk_tile<Ty, s.KT, s.NW, s.CT, NPX, MODE>(a, roles, n, st);
     });
 }

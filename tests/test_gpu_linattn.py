@@ -334,6 +334,20 @@ def test_prompt_then_steps(type_):
     check_forward(c, kw, {"o": torch.cat(outs, 1), "state": state})
 
 
+@pytest.mark.parametrize("type_", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("Dk,Dv", [(20, 72), (64, 128), (128, 128), (100, 130)])
+@pytest.mark.parametrize("seg", [64, 1 << 20])
+def test_many_heads(type_, Dk, Dv, seg, monkeypatch):
+    """Enough heads and segments for the wide blocks of every walk (few heads take narrow ones)."""
+    monkeypatch.setenv("DEER_LIN_SEG", str(seg))
+    B, T = (11, 150) if seg == 64 else (33, 70)
+    lengths = np.linspace(T, 0, B).astype(int)
+    c, kw, g, gs = make(B, T, 4, 2, Dk, Dv, type_, seg == 64, True, lengths)
+    say("linattn many heads", type_, Dk, Dv, seg)
+    check_forward(c, kw)
+    check_adjoint(c, kw, g, gs)
+
+
 @pytest.mark.parametrize("seg", [64, 320])
 def test_state_in_place_over_segments(seg, monkeypatch):
     """state0 overwritten by the state behind the last of 3 or 11 segments, which every block starts from."""
