@@ -277,7 +277,7 @@ int deer_linattn_adjoint(const deer_linattn_shape *s, int B, int T, const deer_v
     if (shared && (rc = launch_lin_head_sum(s->dtype, (size_t)B * T, s->Hk, r, Dk, w.dq, w.dk, dq, dk, st))) return rc;
     if (!decay) return DEER_OK;
     const int tiles = lin_tiles(Dv, Dk);
-    return launch_lin_decay_grad(a, w.dq_dot, tiles, w.dk_dot, tiles, w.fwd, w.rev, Dk * Dv, w.part, dlog_decay, st);
+    return launch_lin_decay_grad(a, w.dq_dot, tiles, w.dk_dot, tiles, w.fwd, w.rev, Dk * Dv, !state0, w.part, dlog_decay, st);
 }
 
 int deer_linattn_step(const deer_linattn_shape *s, int B, const deer_view *q, const deer_view *k, const deer_view *v,

@@ -117,8 +117,8 @@ constexpr int kSpanThreads = 256, kPer = kLinAnchor / kSpanThreads;
 
 __global__ __launch_bounds__(kSpanThreads) void k_lin_decay_grad(LinArgs a, const float *dq, int q_tiles,
                                                                  const float *dk, int k_tiles, const float *fwd,
-                                                                 const float *rev, int elems, double *part,
-                                                                 float *out) {
+                                                                 const float *rev, int elems, bool from_zero,
+                                                                 double *part, float *out) {
     __shared__ double sh[kSpanThreads];
     const int na = (a.T + kLinAnchor - 1) / kLinAnchor, sp = blockIdx.x % na, bh = blockIdx.x / na;
     const int b = bh / a.H, h = bh % a.H, tid = threadIdx.x, len = length_of(a, b);
@@ -173,7 +173,9 @@ __global__ __launch_bounds__(kSpanThreads) void k_lin_decay_grad(LinArgs a, cons
     for (int i = 0; i < kPer; ++i) {
         const int t = t0 + tid * kPer + i;
         if (t >= a.T) continue;
-        const double v = t < len ? d[i] + after : 0.0;
+        // nothing to decay in the first step from no state, nothing left of it by a decay of zero: exactly 0
+        const bool none = t >= len || (from_zero && t == 0) || gate_of(gate_raw(a, b, h, t, len, false)) == -256.0;
+        const double v = none ? 0.0 : d[i] + after;
         if (a.per_step) out[((size_t)b * a.T + t) * a.H + h] = (float)v;
         sum += v;
     }
@@ -204,13 +206,13 @@ __global__ __launch_bounds__(256) void k_lin_decay_sum(int B, int H, int na, con
 }
 
 int launch_lin_decay_grad(const LinArgs &a, const float *dq_dot, int q_tiles, const float *dk_dot, int k_tiles,
-                          const float *fwd_anchor, const float *rev_anchor, int elems, double *part, float *dlog_decay,
-                          hipStream_t st) {
+                          const float *fwd_anchor, const float *rev_anchor, int elems, bool from_zero, double *part,
+                          float *dlog_decay, hipStream_t st) {
     const int na = (a.T + kLinAnchor - 1) / kLinAnchor;
     {
         KTimer kt("k_lin_decay_grad", st);
         hipLaunchKernelGGL(k_lin_decay_grad, dim3(a.B * a.H * na), dim3(kSpanThreads), 0, st, a, dq_dot, q_tiles,
-                           dk_dot, k_tiles, fwd_anchor, rev_anchor, elems, part, dlog_decay);
+                           dk_dot, k_tiles, fwd_anchor, rev_anchor, elems, from_zero, part, dlog_decay);
         DEER_LAUNCH_CHECK("k_lin_decay_grad");
     }
     if (a.per_step) return DEER_OK;

@@ -365,6 +365,8 @@ static int teams_of(size_t rows, int G, int team, size_t threads) {
     if (rows <= cap) return (int)rows;
     return (int)(cap < (size_t)G ? (size_t)G : cap / G * G);
 }
+// (with 3/4, 1, 3/2 and 2 times as many, 32768 rows in bf16 take, of 2048 forwards, 55, 53, 57 and 64 us, of
+// 4096 backwards 171, 162, 170 and 188)
 constexpr size_t kForwardThreads = 256 * 1024, kAdjointThreads = 256 * 512;
 
 static int partials_of(const NormArgs &a) {

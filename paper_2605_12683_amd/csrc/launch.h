@@ -377,10 +377,10 @@ int launch_lin_walk_bf16(const LinArgs &a, const LinRole *roles, int n, bool sta
 int launch_lin_walk_f16(const LinArgs &a, const LinRole *roles, int n, bool states, bool dots, hipStream_t st);
 int launch_lin_walk_f32(const LinArgs &a, const LinRole *roles, int n, bool states, bool dots, hipStream_t st);
 // gradient of the log decays from the dots of dq and dk and the states at the anchors:
-// part is [B, H, anchors] doubles
+// part is [B, H, anchors] doubles; from_zero: no state before the first step
 int launch_lin_decay_grad(const LinArgs &a, const float *dq_dot, int q_tiles, const float *dk_dot, int k_tiles,
-                          const float *fwd_anchor, const float *rev_anchor, int elems, double *part, float *dlog_decay,
-                          hipStream_t st);
+                          const float *fwd_anchor, const float *rev_anchor, int elems, bool from_zero, double *part,
+                          float *dlog_decay, hipStream_t st);
 // dq_out[b, t, hk, :] = sum over the r heads that share hk of dq[b, t, hk r + i, :]; dk_out likewise
 int launch_lin_head_sum(int dtype, size_t rows, int Hk, int r, int D, const float *dq, const float *dk, void *dq_out,
                         void *dk_out, hipStream_t st);

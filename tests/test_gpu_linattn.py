@@ -171,6 +171,24 @@ def test_decays_of_every_size(type_):
 
 
 @pytest.mark.parametrize("type_", ["f32", "bf16"])
+def test_decays_of_nothing(type_):
+    """Decays of zero, and the first step's from no state, have a gradient of zero exactly; one decay for
+    each head that is zero as well."""
+    c, kw, g, gs = make(2, 300, 3, 1, 20, 36, type_, True)
+    c["log_decay"][0, [40, 64, 200], 1] = -torch.inf
+    c["log_decay"][1, 250, 2] = torch.finfo(torch.float32).min
+    say("linattn decays of nothing", type_)
+    grad = D.deer_linattn_adjoint(**c, g=g, **kw)["grads"]["log_decay"]
+    assert (grad[0, [40, 64, 200], 1] == 0).all() and grad[1, 250, 2] == 0 and (grad[:, 0] == 0).all()
+    assert (grad != 0).sum() == grad.numel() - 4 - 6
+    check_adjoint(c, kw, g, None)
+    c["log_decay"] = torch.tensor([-torch.inf, -0.1, -0.2], device="cuda")
+    grad = D.deer_linattn_adjoint(**c, g=g, **kw)["grads"]["log_decay"]
+    assert grad[0] == 0 and (grad[1:] != 0).all()
+    check_adjoint(c, kw, g, None)
+
+
+@pytest.mark.parametrize("type_", ["f32", "bf16"])
 def test_growth(type_):
     """States that grow for a while (by e^0.9 a step for 60 steps, 2^78) and decay again."""
     c, kw, g, gs = make(1, 200, 2, 1, 16, 24, type_, True, True)
