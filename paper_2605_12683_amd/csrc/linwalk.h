@@ -485,7 +485,8 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
     };
     const T *partner = nullptr;
     bool partner_fast = false;
-    if constexpr (DOTS) {
+    const bool dotted = DOTS && ro.dot;                        // (dv's role, beside those of dq and dk, has none)
+    if (dotted) {
         partner = (const T *)ro.partner.p + b * ro.partner.sb + (h / ro.partner.r) * ro.partner.sh;
         const long row = ro.partner.st * (long)sizeof(T);
         partner_fast = (((uintptr_t)partner | (uintptr_t)row) & (4 * CT * sizeof(T) - 1) & 15) == 0 && N % (4 * CT) == 0 &&
@@ -532,7 +533,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
         }
         float *anc = nullptr;
         if constexpr (DOTS) {
-            if ((t0 + C) % kLinAnchor == 0 || t0 + C >= a.T) anc = ro.anchor + ((size_t)bh * na + t0 / kLinAnchor) * mat;
+            if (dotted && ((t0 + C) % kLinAnchor == 0 || t0 + C >= a.T)) anc = ro.anchor + ((size_t)bh * na + t0 / kLinAnchor) * mat;
             if (anc && rev) put_state(anc, N, 1, dc.before);
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -772,7 +773,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
                 }
             }
             if constexpr (DOTS)
-                if (ks == KS - 1) read_partner();
+                if (ks == KS - 1 && dotted) read_partner();
             if constexpr (STATE)
 #pragma unroll
             for (int n = 0; n < DT / KB; ++n) {
@@ -786,7 +787,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
         if (!OUT || DOTS || ahead || keep) finish(std::true_type{});
         else if constexpr (MODE == kOut) finish(std::false_type{});
 
-        if constexpr (DOTS) {
+        if (dotted) {
             const int lane = lane_now(), g = lane >> 4, c = lane & 15;
 #pragma unroll
             for (int it = 0; it < NT; ++it) {
@@ -862,7 +863,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
                     }
             }
         }
-        if constexpr (DOTS) {
+        if (dotted) {
             const int i = threadIdx.x, t = rev ? t0 + C - 1 - i : t0 + i;
             if (i < C && t < a.T) {
                 float d = 0.f;
