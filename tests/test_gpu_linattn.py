@@ -366,6 +366,18 @@ def test_many_heads(type_, Dk, Dv, seg, monkeypatch):
     check_adjoint(c, kw, g, gs)
 
 
+@pytest.mark.parametrize("B,T,H,Hk,Dk,Dv,type_", [(2, 300, 4, 2, 64, 64, "bf16"), (1, 200, 2, 2, 100, 72, "f32"),
+                                                  (2, 130, 3, 1, 32, 128, "f16"), (50, 70, 8, 8, 40, 40, "bf16")])
+def test_adjoint_without_decays(B, T, H, Hk, Dk, Dv, type_):
+    """The other gradients alone; few heads and many."""
+    c, kw, g, gs = make(B, T, H, Hk, Dk, Dv, type_, True, True)
+    say("linattn without decays", B, T, H, Dk, Dv, type_)
+    full = D.deer_linattn_adjoint(**c, g=g, **kw, g_state=gs)["grads"]
+    grads = D.deer_linattn_adjoint(**c, g=g, **kw, g_state=gs, want_decay=False)["grads"]
+    assert set(full) - set(grads) == {"log_decay"}
+    check_adjoint(c, kw, g, gs, {**grads, "log_decay": full["log_decay"]})
+
+
 @pytest.mark.parametrize("seg", [64, 320])
 def test_state_in_place_over_segments(seg, monkeypatch):
     """state0 overwritten by the state behind the last of 3 or 11 segments, which every block starts from."""
