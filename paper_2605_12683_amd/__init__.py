@@ -563,6 +563,7 @@ def deer_linattn(q, k, v, log_decay, *, scale: float = 1.0, lengths=None, state0
     strides (views with a unit last stride are read in place); log_decay float32 [H] or [B, T, H];
     lengths int32 [B] (steps of each sequence; rows behind them are not read and give zeros);
     state0 float32 [B, H, Dk, Dv].  o and state are buffers for the outputs; state may be state0.
+    A NaN or an infinity among the rows that are read may reach any result of its sequence and head.
     Returns dict(o [B, T, H, Dv], state (None unless want_state or a buffer is given))."""
     lib = load()
     a = _Lin(4, q, k, v, log_decay, scale, lengths)
