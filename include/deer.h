@@ -333,7 +333,8 @@ int deer_readout_loss(const deer_readout *readout, int B, int T, int M, const fl
  * As for the diagonal SSM, deer_linattn computes every step of the sequence in parallel
  * (chunks of steps as matrix products, the chunks joined by their decays), the adjoint is the
  * same recurrence run backwards, and deer_linattn_step is the recurrence itself for one step
- * (generation).  States, decays and every sum are float32 whatever the operands' type. */
+ * (generation).  States, decays and every sum are float32 whatever the operands' type, what one
+ * product leaves for the next keeps float32's 24 bits, and a result is rounded to its type once. */
 enum { DEER_F32 = 0, DEER_BF16 = 1, DEER_F16 = 2 };
 
 typedef struct {

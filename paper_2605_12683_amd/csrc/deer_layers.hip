@@ -268,7 +268,7 @@ int deer_linattn_adjoint(const deer_linattn_shape *s, int B, int T, const deer_v
         ro[1].seg = w.rseg, ro[1].seg_decay = w.rseg_decay;
         ro[1].seg_d = 1, ro[1].seg_n = Dv;                       // R^T: the same states, read across
     }
-    // Dots that are summed over up to kLinAnchor steps take the finer products; dv by itself need not, but
+    // The walk that leaves dots and anchors takes longer for a chunk; dv has none and runs by itself, but
     // goes along where all blocks are resident at once (1 x 200 steps, 8 heads of 128 x 128 in bf16: 55 us
     // apart, 41 together; with more blocks it would wait for theirs: 64 heads of 4096 steps, dq and dk 188
     // us, dv by itself 94 for 256 of 768 blocks).

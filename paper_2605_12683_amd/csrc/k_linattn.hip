@@ -86,10 +86,10 @@ int lin_tiles(int Kd, int N) {
 
 int lin_resident(int dtype, int Kd, int N, bool dots) {
     return with_dtype(dtype, [&](auto ty) {
-        constexpr int NPI = InParts<decltype(ty)>::n, NPX = NPI == 3 ? 3 : 2;
+        constexpr int NPI = InParts<decltype(ty)>::n;
         return with_walk_shape<NPI>(Kd, N, false, [&](auto s) {
-            return dots ? LinTile<NPI, s.KT, s.NW, s.CT, 3, kOutDots>::waves * 4 / s.NW
-                        : LinTile<NPI, s.KT, s.NW, s.CT, NPX, kOut>::waves * 4 / s.NW;
+            return dots ? LinTile<NPI, s.KT, s.NW, s.CT, kOutDots>::waves * 4 / s.NW
+                        : LinTile<NPI, s.KT, s.NW, s.CT, kOut>::waves * 4 / s.NW;
         });
     });
 }

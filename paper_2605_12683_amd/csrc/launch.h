@@ -368,8 +368,7 @@ int lin_tiles(int Kd, int N);   // blocks that share the N columns of one head's
 int lin_resident(int dtype, int Kd, int N, bool dots);   // a walk's blocks per CU
 bool lin_same_tile(int Kd, int N, int Kd2, int N2);
 // all roles of one call have the same tile shape; states: what each segment adds (into seg,
-// seg_decay), else the outputs; dots: and dot, anchor (which are summed over many steps, so the
-// intermediate values of 16-bit operands then take 24 bits, not 16)
+// seg_decay), else the outputs; dots: and dot, anchor
 int launch_lin_walk(const LinArgs &a, const LinRole *roles, int nroles, bool states, bool dots, hipStream_t st);
 // seg from what each segment adds to the state entering it
 int launch_lin_join(const LinArgs &a, const LinRole *roles, int nroles, hipStream_t st);

@@ -10,9 +10,10 @@
 //
 // Products run on the bf16 matrix cores with float32 sums.  Operands of fewer bits enter exactly: a
 // bf16 number as it is, an fp16 number as two bf16 parts, a float32 number as three (split16.h).
-// What is formed in between is split likewise, into NPX parts where it meets the outputs (two: 16
-// bits, for 16-bit outputs, 2^8 times finer than their own rounding; three: float32's 24) and always
-// into three where it enters the state, which is float32 for as long as the sequence lasts.
+// What is formed in between (the decayed scores, the entering state, v times its decay) is float32 and
+// enters the next product in three parts, which hold all its 24 bits whatever the operands' type. (Two
+// parts where it meets 16-bit outputs would be 3 to 6% faster in bf16 and 5 to 12% in fp16, but flip
+// the last bit of 0.24% and 2.3% of the outputs against sums in float32.)
 //
 // One block of NW waves walks one head's chunks for NB = 16 NW CT columns of the state; a wave keeps
 // its 16 CT columns in registers for the whole walk, as matrix-core accumulators.  Their lane layout
@@ -89,7 +90,7 @@ constexpr int nb_of(int KT, int N) { return N > 64 && KT <= 128 ? 128 : 64; }
 // states at the anchors
 enum { kStates = 0, kOut = 1, kOutDots = 2 };
 
-template <int NPI, int KT, int NW, int CT, int NPX, int MODE>   // waves, 16-column tiles per wave
+template <int NPI, int KT, int NW, int CT, int MODE>   // waves, 16-column tiles per wave
 struct LinTile {
     static constexpr bool OUT = MODE != kStates;
     static constexpr int NB = 16 * NW * CT, TH = 64 * NW;
@@ -100,7 +101,7 @@ struct LinTile {
     static constexpr int PQ = KT + 16, PK = KT + 16, PV = NB + 16;
     static constexpr int pairs(int C) { return C == 64 ? 6 : 2; }   // (16 outputs, 32 sources) not all above the diagonal
     static constexpr int bytes(int C) {
-        return NPI * C * 2 * ((OUT ? PQ : 0) + PK + PV) + (OUT ? pairs(C) * NPX * 1024 : 0) + 2 * (4 * C + 4) * 4 +
+        return NPI * C * 2 * ((OUT ? PQ : 0) + PK + PV) + (OUT ? pairs(C) * 3 * 1024 : 0) + 2 * (4 * C + 4) * 4 +
                (MODE == kOutDots ? NW * C * 4 : 0);
     }
     static constexpr int C = bytes(64) <= 80 * 1024 ? 64 : 32;
@@ -265,21 +266,14 @@ __device__ __forceinline__ v2u read_turned(const uint16_t *p) {
         v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)p));
 }
 
-// the first NP parts of eight floats, as one operand each
-template <int NP>
-__device__ __forceinline__ void split8(const float (&x)[8], v4u (&p)[NP]) {
+// the three parts of eight floats, as one operand each
+__device__ __forceinline__ void split8(const float (&x)[8], v4u (&p)[3]) {
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-        float x0 = x[2 * w], x1 = x[2 * w + 1];
+        uint32_t s[3];
+        split_pair(x[2 * w], x[2 * w + 1], s);
 #pragma unroll
-        for (int q = 0; q < NP; ++q) {
-            const uint32_t s = cvt_pair(x0, x1);
-            p[q][w] = s;
-            if (q + 1 < NP) {
-                x0 -= __uint_as_float(s << 16);
-                x1 -= __uint_as_float(s & 0xffff0000u);
-            }
-        }
+        for (int q = 0; q < 3; ++q) p[q][w] = s[q];
     }
 }
 
@@ -296,12 +290,12 @@ __device__ __forceinline__ v4f mfma_parts(const v4u (&x)[NA], const v4u (&y)[NB]
     return acc;
 }
 
-// the same of every pair of X and Y operands, acc(x, y) += x y, so that consecutive products belong
-// to different sums
-template <int LIM, int X, int Y, int NA, int NB, class Acc>
+// the same (up to 2) of every pair of X and Y operands, acc(x, y) += x y, so that consecutive products
+// belong to different sums
+template <int X, int Y, int NA, int NB, class Acc>
 __device__ __forceinline__ void mfma_block(const v4u (&x)[X][NA], const v4u (&y)[Y][NB], Acc acc) {
 #pragma unroll
-    for (int s = LIM; s >= 0; --s)
+    for (int s = 2; s >= 0; --s)
 #pragma unroll
         for (int p = 0; p < NA; ++p) {
             const int q = s - p;
@@ -372,11 +366,11 @@ __device__ __forceinline__ double chunk_decays(Decays<C> &d, float raw, float sc
 
 // ---- the walk ---------------------------------------------------------------------------------
 
-template <class Ty, int KT, int NW, int CT, int NPX, int MODE>
-__global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, MODE>::waves)) void k_lin_walk(LinArgs a,
-                                                                                                              LinRoles rs) {
+template <class Ty, int KT, int NW, int CT, int MODE>
+__global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, MODE>::waves)) void k_lin_walk(LinArgs a,
+                                                                                                         LinRoles rs) {
     constexpr int NPI = InParts<Ty>::n;
-    using Tile = LinTile<NPI, KT, NW, CT, NPX, MODE>;
+    using Tile = LinTile<NPI, KT, NW, CT, MODE>;
     using T = typename Ty::T;
     constexpr bool OUT = Tile::OUT, DOTS = MODE == kOutDots;
     constexpr int C = Tile::C, NB = Tile::NB, TH = Tile::TH, PQ = Tile::PQ, PK = Tile::PK, PV = Tile::PV;
@@ -384,14 +378,14 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
     // operands read from LDS at a time: as many as the registers hold twice (dividing KT / 32, NT, DT)
     constexpr bool TIGHT = KT == 128 && Tile::waves == 4;
     constexpr int UB = TIGHT || NPI == 3 || KT == 32 ? 1 : 2;
-    constexpr int QB = TIGHT || CT == 2 || KT == 256 ? 2 : NT, KB = NPI == 1 && !TIGHT && DT > 2 ? 4 : 2, PB = NPX == 2 && !TIGHT ? 2 : 1;
+    constexpr int QB = TIGHT || CT == 2 || KT == 256 ? 2 : NT, KB = NPI == 1 && !TIGHT && DT > 2 ? 4 : 2;
     extern __shared__ __align__(16) unsigned char smem[];
     uint16_t *Ks = (uint16_t *)smem, *Vs = Ks + NPI * C * PK, *Qs = Vs + NPI * C * PV;
     unsigned char *rest = (unsigned char *)(Qs + (OUT ? NPI * C * PQ : 0));
     constexpr int PAIRS = Tile::pairs(C);
-    v4u *Ps = (v4u *)rest;                                     // [PAIRS][NPX][64 lanes]
+    v4u *Ps = (v4u *)rest;                                     // [PAIRS][3][64 lanes]
     auto pair = [](int it, int ks) { return it < 2 ? it : 2 * it - 2 + ks; };
-    Decays<C> *dec = (Decays<C> *)(rest + (OUT ? PAIRS * NPX * 1024 : 0));
+    Decays<C> *dec = (Decays<C> *)(rest + (OUT ? PAIRS * 3 * 1024 : 0));
     float *dots = (float *)(dec + 2);                          // [NW][C]
 
     const LinRole ro = rs.r[blockIdx.y];
@@ -495,7 +489,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
 
     // the tile above the diagonal that shares an operand with the first stays zero
     if constexpr (OUT && C == 32)
-        for (int i = threadIdx.x; i < PAIRS * NPX * 64; i += TH) Ps[i] = v4u{0, 0, 0, 0};
+        for (int i = threadIdx.x; i < PAIRS * 3 * 64; i += TH) Ps[i] = v4u{0, 0, 0, 0};
     auto store = [&] {
         kr.template store<false, OUT>(Ks, PK);
         vr.template store<false, false>(Vs, PV);
@@ -598,9 +592,9 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
                     split_pair(x[0], x[1], pp[m][0]);
                     split_pair(x[2], x[3], pp[m][1]);
                 }
-                auto operand = [&](int m) { return Ps + pair(it[m], jt[m] >> 1) * NPX * 64 + lane; };
+                auto operand = [&](int m) { return Ps + pair(it[m], jt[m] >> 1) * 3 * 64 + lane; };
 #pragma unroll
-                for (int q = 0; q < NPX; ++q) {
+                for (int q = 0; q < 3; ++q) {
                     if constexpr (TWO) operand(0)[q * 64] = v4u{pp[0][0][q], pp[0][1][q], pp[1][0][q], pp[1][1][q]};
                     else *((v2u *)(operand(0) + q * 64) + (jt[0] & 1)) = v2u{pp[0][0][q], pp[0][1][q]};
                     if constexpr (M > 2) operand(2)[q * 64] = v4u{pp[2][0][q], pp[2][1][q], 0, 0};   // (above the diagonal)
@@ -630,7 +624,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
             };
             constexpr int QN = KT / 32 * (NT / QB);
             read_q(0);
-            v4u sf[CT][NPX];
+            v4u sf[CT][3];
 #pragma unroll
             for (int n = 0; n < QN; ++n) {
                 const int u = n / (NT / QB), it0 = n % (NT / QB) * QB;
@@ -642,9 +636,9 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
                         float x[8];
 #pragma unroll
                         for (int r = 0; r < 4; ++r) x[r] = S[2 * u][ct][r], x[4 + r] = S[2 * u + 1][ct][r];
-                        split8<NPX>(x, sf[ct]);
+                        split8(x, sf[ct]);
                     }
-                mfma_block<NPX - 1, CT, QB>(sf, qf[n & 1], [&](int ct, int m) -> v4f & { return O[it0 + m][ct]; });
+                mfma_block<CT, QB>(sf, qf[n & 1], [&](int ct, int m) -> v4f & { return O[it0 + m][ct]; });
                 __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
@@ -720,15 +714,10 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
                     const v2u v1 = read_turned(vp + (ks * 32 + 16 + 4 * g + (c >> 2)) * PV);
                     vf[ct][p] = v4u{v0[0], v0[1], v1[0], v1[1]};
                 }
-            v4u pf[2][PB][NPX], kf[2][KB][NPI];   // the operands of the next products read while these run
-            auto read_p = [&](int n) {
+            v4u pf[2][1][3], kf[2][KB][NPI];   // the operands of the next products read while these run
+            auto read_p = [&](int it) {
 #pragma unroll
-                for (int m = 0; m < PB; ++m) {
-                    const int it = 2 * ks + n * PB + m;
-                    if (it < NT)
-#pragma unroll
-                        for (int q = 0; q < NPX; ++q) pf[n & 1][m][q] = Ps[(pair(it, ks) * NPX + q) * 64 + lane];
-                }
+                for (int q = 0; q < 3; ++q) pf[it & 1][0][q] = Ps[(pair(it, ks) * 3 + q) * 64 + lane];
             };
             auto read_k = [&](int n) {
 #pragma unroll
@@ -741,7 +730,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
                         kf[n & 1][m][p] = v4u{k0[0], k0[1], k1[0], k1[1]};
                     }
             };
-            if constexpr (OUT) read_p(0);
+            if constexpr (OUT) read_p(2 * ks);
             else read_k(0);
             __builtin_amdgcn_sched_barrier(0);
             if constexpr (STATE)
@@ -758,17 +747,16 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
                     }
 #pragma unroll
                 for (int r = 0; r < 4; ++r) x[r] *= into0[r], x[4 + r] *= into1[r];
-                split8<3>(x, sv[ct]);
+                split8(x, sv[ct]);
             }
             if constexpr (OUT) {
-                constexpr int PN = (NT + PB - 1) / PB;
 #pragma unroll
-                for (int n = 0; n < PN; ++n) {
-                    if (2 * ks + n * PB >= NT) break;
-                    if (2 * ks + (n + 1) * PB < NT) read_p(n + 1);
+                for (int it = 0; it < NT; ++it) {
+                    if (it < 2 * ks) continue;                 // (all of its sources lie above the diagonal)
+                    if (it + 1 < NT) read_p(it + 1);
                     else if (STATE) read_k(0);
                     __builtin_amdgcn_sched_barrier(0);
-                    mfma_block<NPX - 1, CT, PB>(vf, pf[n & 1], [&](int ct, int m) -> v4f & { return O[2 * ks + n * PB + m][ct]; });
+                    mfma_block<CT, 1>(vf, pf[it & 1], [&](int ct, int) -> v4f & { return O[it][ct]; });
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
@@ -779,7 +767,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
             for (int n = 0; n < DT / KB; ++n) {
                 if (n + 1 < DT / KB) read_k(n + 1);
                 __builtin_amdgcn_sched_barrier(0);
-                mfma_block<2, KB, CT>(kf[n & 1], sv, [&](int m, int ct) -> v4f & { return S[n * KB + m][ct]; });
+                mfma_block<KB, CT>(kf[n & 1], sv, [&](int m, int ct) -> v4f & { return S[n * KB + m][ct]; });
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
@@ -888,9 +876,9 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, NPX, 
 
 // ---- launches -------------------------------------------------------------------------------------
 
-template <class Ty, int KT, int NW, int CT, int NPX, int MODE>
+template <class Ty, int KT, int NW, int CT, int MODE>
 int launch_walk_tile(const LinArgs &a, const LinRole *roles, int n, hipStream_t st) {
-    using Tile = LinTile<InParts<Ty>::n, KT, NW, CT, NPX, MODE>;
+    using Tile = LinTile<InParts<Ty>::n, KT, NW, CT, MODE>;
     LinRoles rs{};
     int tiles = 0;
     for (int i = 0; i < n; ++i) {
@@ -898,17 +886,17 @@ int launch_walk_tile(const LinArgs &a, const LinRole *roles, int n, hipStream_t 
         const int t = (roles[i].N + Tile::NB - 1) / Tile::NB;
         tiles = t > tiles ? t : tiles;
     }
-    const void *fn = (const void *)k_lin_walk<Ty, KT, NW, CT, NPX, MODE>;
+    const void *fn = (const void *)k_lin_walk<Ty, KT, NW, CT, MODE>;
     if (Tile::lds > 64 * 1024) DEER_HIP(hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, Tile::lds));
     KTimer kt(MODE == kStates ? "k_lin_walk_states" : "k_lin_walk", st);
-    hipLaunchKernelGGL((k_lin_walk<Ty, KT, NW, CT, NPX, MODE>), dim3((unsigned)(a.B * a.H * a.nseg * tiles), n),
+    hipLaunchKernelGGL((k_lin_walk<Ty, KT, NW, CT, MODE>), dim3((unsigned)(a.B * a.H * a.nseg * tiles), n),
                        dim3(64 * NW), Tile::lds, st, a, rs);
     DEER_LAUNCH_CHECK("k_lin_walk");
     return DEER_OK;
 }
 
-template <class Ty, int NPX, int MODE>
-int launch_walk_parts(const LinArgs &a, const LinRole *roles, int n, hipStream_t st) {
+template <class Ty, int MODE>
+int launch_walk_mode(const LinArgs &a, const LinRole *roles, int n, hipStream_t st) {
     // Where blocks of 128 columns leave half of the CUs without one, twice as many of 64, which take less
     // time for a chunk (1 x 2048 steps, 4 heads of 128 x 128 in bf16: 33 us, narrow 27; with up to 256
     // blocks the second reading of q and k costs more: 64 heads' adjoint 382, narrow 397).  Not with dots,
@@ -916,8 +904,14 @@ int launch_walk_parts(const LinArgs &a, const LinRole *roles, int n, hipStream_t
     const int nb = nb_of(kt_of(roles[0].Kd), roles[0].N), tiles = (roles[0].N + nb - 1) / nb;
     const bool narrow = MODE != kOutDots && nb == 128 && (long)a.B * a.H * a.nseg * tiles * n <= 128;
     return with_walk_shape<InParts<Ty>::n>(roles[0].Kd, roles[0].N, narrow, [&](auto s) {
-        return launch_walk_tile<Ty, s.KT, s.NW, s.CT, NPX, MODE>(a, roles, n, st);
+        return launch_walk_tile<Ty, s.KT, s.NW, s.CT, MODE>(a, roles, n, st);
     });
+}
+
+template <class Ty>
+int launch_walk_type(const LinArgs &a, const LinRole *roles, int n, bool states, bool dots, hipStream_t st) {
+    if (states) return launch_walk_mode<Ty, kStates>(a, roles, n, st);
+    return dots ? launch_walk_mode<Ty, kOutDots>(a, roles, n, st) : launch_walk_mode<Ty, kOut>(a, roles, n, st);
 }
 
 }  // namespace deer

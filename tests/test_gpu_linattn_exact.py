@@ -1,0 +1,78 @@
+"""Linear attention on the GPU where float32 arithmetic is exact: operands on a grid so coarse that
+every product and every sum of magnitudes has at most 24 bits, decays of one.  However the sums are
+ordered, a result is then the exact one rounded once to its type, and is compared bit for bit."""
+import numpy as np
+import pytest
+
+from gpu_util import say
+from oracle import layers as L
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():
+    pytest.skip("needs a GPU", allow_module_level=True)
+
+import paper_2605_12683_amd as D  # noqa: E402
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+GRID = 2.0 ** -10       # of every result
+MOST = 8                # elements of a row that are not zero
+
+
+def rows(rng, shape, wide):
+    """1, 0 or -1, or 7-bit numbers of two sizes (products of 10 to 20 bits of the grid); at most MOST of
+    each row are not zero."""
+    x = rng.integers(-127, 128, shape) * rng.choice([2.0 ** -5, 2.0 ** -2], shape) if wide else \
+        rng.integers(-1, 2, shape).astype(np.float64)
+    x[rng.random(shape).argsort(-1) >= MOST] = 0.0
+    return x
+
+
+def rounded(x, type_):
+    assert (np.abs(x) < 2.0 ** 24 * GRID).all() and (x == np.rint(x / GRID) * GRID).all()
+    return torch.tensor(x).float().to(type_).cuda()       # float32 holds it, so this rounds once
+
+
+def same(name, got, want):
+    off = int((got != want).sum())
+    assert off == 0, (name, off, got.numel())
+
+
+@pytest.mark.parametrize("type_", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("B,T,H,Hk,Dk,Dv", [(16, 6, 4, 2, 16, 24), (1, 70, 8, 8, 64, 64), (40, 40, 8, 4, 64, 128),
+                                            (1, 9, 2, 2, 256, 256), (17, 33, 16, 8, 128, 128)])
+@pytest.mark.parametrize("large", ["states", "q and k", "v and g"])
+def test_rounded_once(type_, B, T, H, Hk, Dk, Dv, large):
+    """States of 20 bits, then scores q k and v g of as many, on their way to outputs of 8, 11 or 24:
+    none is rounded in between."""
+    say("linattn rounded once", type_, B, T, H, Hk, Dk, Dv, large)
+    rng = np.random.default_rng(B + T + Dv)
+    q, k = (rows(rng, (B, T, Hk, Dk), large == "q and k") for _ in range(2))
+    v, g = (rows(rng, (B, T, H, Dv), large == "v and g") for _ in range(2))
+    s0 = gs = None
+    if large == "states":
+        s0, gs = (rng.integers(-2 ** 19, 2 ** 19, (B, H, Dk, Dv)) * GRID for _ in range(2))
+    ld = np.zeros(H)
+    t = TYPES[type_]
+    dev = {n: torch.tensor(x).to(t).cuda() for n, x in (("q", q), ("k", k), ("v", v))}
+    dev["log_decay"] = torch.zeros(H, device="cuda")
+    dg = torch.tensor(g).to(t).cuda()
+    d0, dgs = (None if x is None else torch.tensor(x).float().cuda() for x in (s0, gs))
+    # every sum of magnitudes stays within 24 bits
+    mags = [None if x is None else np.abs(x) for x in (q, k, v, g, s0, gs)]
+    oa, _ = L.linattn(*mags[:3], ld, state0=mags[4])
+    ga = L.linattn_adjoint(*mags[:3], ld, mags[3], state0=mags[4], g_state=mags[5])
+    assert all((x < 2.0 ** 24 * GRID).all() for x in (oa, ga["q"], ga["k"], ga["v"]))
+
+    o, last = L.linattn(q, k, v, ld, state0=s0)
+    r = D.deer_linattn(**dev, state0=d0, want_state=True)
+    same("o", r["o"], rounded(o, t))
+    same("state", r["state"], rounded(last, torch.float32))
+    ref = L.linattn_adjoint(q, k, v, ld, g, state0=s0, g_state=gs)
+    for want_decay in (True, False):
+        got = D.deer_linattn_adjoint(**dev, g=dg, state0=d0, g_state=dgs, want_decay=want_decay)["grads"]
+        for n in ("q", "k", "v"):
+            same(n, got[n], rounded(ref[n], t))
+        if s0 is not None:
+            same("state0", got["state0"], rounded(ref["state0"], torch.float32))
