@@ -12,8 +12,8 @@
 // bf16 number as it is, an fp16 number as two bf16 parts, a float32 number as three (split16.h).
 // What is formed in between (the decayed scores, the entering state, v times its decay) is float32 and
 // enters the next product in three parts, which hold all its 24 bits whatever the operands' type. (Two
-// parts where it meets 16-bit outputs would be 3 to 6% faster in bf16 and 5 to 12% in fp16, but flip
-// the last bit of 0.24% and 2.3% of the outputs against sums in float32.)
+// parts where it meets 16-bit outputs would save up to 8% of the time in bf16 and 12% in fp16, but flip
+// the last bit of 0.24% of the outputs in bf16, and of over 1% in fp16, against sums in float32.)
 //
 // One block of NW waves walks one head's chunks for NB = 16 NW CT columns of the state; a wave keeps
 // its 16 CT columns in registers for the whole walk, as matrix-core accumulators.  Their lane layout
@@ -277,11 +277,12 @@ __device__ __forceinline__ void split8(const float (&x)[8], v4u (&p)[3]) {
     }
 }
 
-// acc += sum of the products of parts whose indices add up to at most LIM, the smallest first
-template <int LIM, int NA, int NB>
+// acc += sum of the products of parts whose indices add up to at most 2, the smallest first: all of
+// operands of one and two parts, and of three parts all but those below 2^-23 of the whole
+template <int NA, int NB>
 __device__ __forceinline__ v4f mfma_parts(const v4u (&x)[NA], const v4u (&y)[NB], v4f acc) {
 #pragma unroll
-    for (int s = LIM; s >= 0; --s)
+    for (int s = 2; s >= 0; --s)
 #pragma unroll
         for (int p = 0; p < NA; ++p) {
             const int q = s - p;
@@ -290,7 +291,7 @@ __device__ __forceinline__ v4f mfma_parts(const v4u (&x)[NA], const v4u (&y)[NB]
     return acc;
 }
 
-// the same (up to 2) of every pair of X and Y operands, acc(x, y) += x y, so that consecutive products
+// the same of every pair of X and Y operands, acc(x, y) += x y, so that consecutive products
 // belong to different sums
 template <int X, int Y, int NA, int NB, class Acc>
 __device__ __forceinline__ void mfma_block(const v4u (&x)[X][NA], const v4u (&y)[Y][NB], Acc acc) {
@@ -576,7 +577,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, MODE>
 #pragma unroll
                     for (int u = 0; u < UB; ++u)
 #pragma unroll
-                        for (int m = 0; m < M; ++m) acc[m] = mfma_parts<NPI - 1>(kf[m][u], qf[m == 1 ? 0 : m][u], acc[m]);
+                        for (int m = 0; m < M; ++m) acc[m] = mfma_parts(kf[m][u], qf[m == 1 ? 0 : m][u], acc[m]);
                 }
                 uint32_t pp[M][2][3];
 #pragma unroll

@@ -76,3 +76,33 @@ def test_rounded_once(type_, B, T, H, Hk, Dk, Dv, large):
             same(n, got[n], rounded(ref[n], t))
         if s0 is not None:
             same("state0", got["state0"], rounded(ref["state0"], torch.float32))
+
+
+def odd(rng, top, *shape):
+    """Odd whole numbers of either sign in the upper half of 1..top: every bit of the type is used."""
+    return (rng.integers(top // 4, top // 2, shape) * 2 + 1) * rng.choice([-1.0, 1.0], shape)
+
+
+@pytest.mark.parametrize("type_,top", [("bf16", 255), ("f16", 2047)])
+@pytest.mark.parametrize("B,H", [(1, 16), (64, 64)])
+def test_whole_products(type_, top, B, H):
+    """Two steps of one row and column, operands of all their bits, decays of one: scores of 22 bits,
+    and the gradient of the second step's decay, which is scale q_2 g_2 k_1 v_1, to the last bit."""
+    say("linattn whole products", type_, B, H)
+    rng = np.random.default_rng(B)
+    scale = 2.0 ** -12
+    t = TYPES[type_]
+    ld = np.zeros((B, 2, H))
+    for pair in (("q", "k"), ("v", "g")):
+        x = {n: odd(rng, top, B, 2, H, 1) if n in pair else rng.choice([-1.0, 1.0], (B, 2, H, 1)) for n in "qkvg"}
+        dev = {n: torch.tensor(y).to(t).cuda() for n, y in x.items()}
+        g = dev.pop("g")
+        dev["log_decay"] = torch.zeros(B, 2, H, device="cuda")
+        # (sums of at most two products of 22 bits)
+        o, last = L.linattn(x["q"], x["k"], x["v"], ld, scale=scale)
+        r = D.deer_linattn(**dev, scale=scale, want_state=True)
+        ref = L.linattn_adjoint(x["q"], x["k"], x["v"], ld, x["g"], scale=scale)
+        got = D.deer_linattn_adjoint(**dev, g=g, scale=scale)["grads"]
+        for name, a, want in (("o", r["o"], o), ("state", r["state"], last), *((n, got[n], ref[n]) for n in "qkv"),
+                              ("log_decay", got["log_decay"], ref["log_decay"])):
+            same(name, a, torch.tensor(want).float().to(a.dtype).cuda())
