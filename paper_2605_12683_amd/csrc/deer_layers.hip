@@ -96,8 +96,8 @@ struct LinWs {
     float *dq_dot, *dk_dot;      // [tiles][B, H, T]
     float *fwd, *rev;            // states at the anchors [B, H, anchors][Dv, Dk]
     double *part;                // [B, H, anchors]
-    float *seg, *seg_decay;      // [B, H, segments] of the forward state (the adjoint: S^T) ...
-    float *rseg, *rseg_decay;    // ... and of R
+    float *seg, *rseg;           // [B, H, segments] of the forward state (the adjoint: S^T), and of R
+    SegDecay *seg_decay, *rseg_decay;
     size_t bytes;
 };
 
@@ -122,10 +122,10 @@ static LinWs carve_lin(void *ws, const deer_linattn_shape *s, int B, int T, int 
     if (steps < T) {
         const size_t n = (size_t)B * s->H * ((T + steps - 1) / steps);
         w.seg = c.take<float>(n * s->Dk * s->Dv);
-        w.seg_decay = c.take<float>(n);
+        w.seg_decay = c.take<SegDecay>(n);
         if (op == DEER_OP_ADJOINT) {
             w.rseg = c.take<float>(n * s->Dk * s->Dv);
-            w.rseg_decay = c.take<float>(n);
+            w.rseg_decay = c.take<SegDecay>(n);
         }
     }
     w.bytes = c.off;

@@ -34,10 +34,11 @@ __global__ __launch_bounds__(256) void k_lin_join(LinArgs a, LinRoles rs) {
             S[r] = ro.init[(size_t)bh * mat + (size_t)d * ro.init_d + (size_t)n * ro.init_n];
         }
     float *seg = ro.seg + (size_t)bh * a.nseg * mat + e;
-    const float *dec = ro.seg_decay + (size_t)bh * a.nseg;
+    const SegDecay *dec = ro.seg_decay + (size_t)bh * a.nseg;
     constexpr int U = 8;
     for (int i0 = 0; i0 < a.nseg; i0 += U) {
-        float x[U][4], f[U];
+        float x[U][4];
+        SegDecay f[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int i = i0 + u, s = ro.reverse ? a.nseg - 1 - i : i;
@@ -49,7 +50,7 @@ __global__ __launch_bounds__(256) void k_lin_join(LinArgs a, LinRoles rs) {
             for (int r = 0; r < 4; ++r) x[u][r] = y[r];
             if (on && !four)
                 for (int r = 0; r < left; ++r) x[u][r] = p[r];
-            f[u] = on ? dec[s] : 0.f;
+            f[u] = on ? dec[s] : SegDecay{0.f, 0};
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -60,7 +61,7 @@ __global__ __launch_bounds__(256) void k_lin_join(LinArgs a, LinRoles rs) {
             else
                 for (int r = 0; r < left; ++r) p[r] = S[r];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) S[r] = fmaf(f[u], S[r], x[u][r]);
+            for (int r = 0; r < 4; ++r) S[r] = decayed(f[u], S[r], x[u][r]);
         }
     }
 }

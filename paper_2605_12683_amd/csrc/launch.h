@@ -333,6 +333,12 @@ struct LinView {
     long sb, st, sh;
     int r;                      // heads of the result that share one head of this operand
 };
+// decay of a segment, factor 2^exponent with a factor of 1 to 2: over many growing steps it passes the
+// range of a float32, while the states that it multiplies, zero or tiny, need not
+struct SegDecay {
+    float factor;
+    int exponent;
+};
 // one walk of the recurrence S = exp(gate) S + sc_kv k v^T, out = sc_o q^T S over [B, T, H]: the
 // forward pass and each gradient of its adjoint are walks with the operands in other places
 struct LinRole {
@@ -352,7 +358,8 @@ struct LinRole {
     bool wide_out;              // N is a multiple of 8 and out lies on 16 bytes
     // walks in segments: what each but the last adds by itself, or (joined) the state entering each:
     // [B, H, segments] matrices, element (d, n) at d seg_d + n seg_n, and the segments' decays
-    float *seg, *seg_decay;
+    float *seg;
+    SegDecay *seg_decay;
     int seg_d, seg_n;
 };
 constexpr int kLinAnchor = 1024;   // steps between the states kept for the gradient of the decays

@@ -68,6 +68,18 @@ __device__ __forceinline__ int length_of(const LinArgs &a, int b) {
     return n < 0 ? 0 : (n > a.T ? a.T : n);
 }
 
+// x + decay S.  S 2^exponent is exact, and no further from zero than the product: zero stays zero, and
+// nothing overflows that the product does not.
+__device__ __forceinline__ float decayed(SegDecay decay, float S, float x) {
+    return fmaf(decay.factor, __builtin_amdgcn_ldexpf(S, decay.exponent), x);
+}
+
+// 2^total (exponents beyond +-1000 make every float32 infinite or zero, and so do these)
+__device__ __forceinline__ SegDecay seg_decay_of(double total) {
+    const double whole = floor(total);
+    return {__builtin_amdgcn_exp2f((float)(total - whole)), (int)fmin(fmax(whole, -1000.0), 1000.0)};
+}
+
 // ---- tile shapes -------------------------------------------------------------------------------
 
 template <class Ty>
@@ -436,14 +448,22 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, MODE>
     };
     {
         const int l = threadIdx.x & 63;
-        auto add_to = [&](float f, const float *src, int sd, int sn) {   // S = f S + src
+        auto add_to = [&](SegDecay f, const float *src, int sd, int sn) {   // S = f S + src
             const auto rsrc = bounded_rsrc(src, src ? (uint32_t)(mat * 4) : 0u);
+            v4f x[DT][CT];
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) S[dt][ct][r] = fmaf(f, S[dt][ct][r], bload(rsrc, at(l, dt, ct, r, sd, sn), 0));
+                    for (int r = 0; r < 4; ++r) x[dt][ct][r] = bload(rsrc, at(l, dt, ct, r, sd, sn), 0);
+            __builtin_amdgcn_sched_barrier(0);                 // (all loads in flight before the first is used)
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) S[dt][ct][r] = decayed(f, S[dt][ct][r], x[dt][ct][r]);
         };
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
@@ -451,8 +471,8 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, MODE>
             for (int ct = 0; ct < CT; ++ct) S[dt][ct] = v4f{0.f, 0.f, 0.f, 0.f};
         if constexpr (OUT) {
             const float *own = ro.seg + ((size_t)bh * a.nseg + seg) * mat;
-            if (a.joined) add_to(0.f, own, ro.seg_d, ro.seg_n);
-            else add_to(0.f, ro.init ? ro.init + bh * mat : nullptr, ro.init_d, ro.init_n);
+            if (a.joined) add_to({0.f, 0}, own, ro.seg_d, ro.seg_n);
+            else add_to({0.f, 0}, ro.init ? ro.init + bh * mat : nullptr, ro.init_d, ro.init_n);
             if (!a.joined)                                     // the segments before this one
                 for (int s = rev ? a.nseg - 1 : 0; s != seg; s += rev ? -1 : 1)
                     add_to(ro.seg_decay[(size_t)bh * a.nseg + s], own + ((long)s - seg) * (long)mat, ro.seg_d, ro.seg_n);
@@ -871,7 +891,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, MODE>
     } else {
         put_state(ro.seg + ((size_t)bh * a.nseg + seg) * mat, N, 1, dec[(chunks - 1) & 1].after);
         if (w == NW - 1 && (threadIdx.x & 63) == 0 && tile == 0)
-            ro.seg_decay[(size_t)bh * a.nseg + seg] = __builtin_amdgcn_exp2f((float)total);
+            ro.seg_decay[(size_t)bh * a.nseg + seg] = seg_decay_of(total);
     }
 }
 
