@@ -546,10 +546,17 @@ class _Lin:
         return _scratch(ws, self.v, need)
 
 
+def _wide(bits, *sizes):
+    """Whether one is negative or has more bits (ctypes would drop them)."""
+    return any(n >> bits for n in sizes)
+
+
 def deer_linattn_workspace_bytes(B: int, T: int, H: int, Hk: int, Dk: int, Dv: int, op: int,
                                  dtype=torch.float32) -> int:
     """Workspace of deer_linattn (op DEER_OP_SOLVE) or deer_linattn_adjoint (DEER_OP_ADJOINT); 0 for
     arguments they refuse."""
+    if dtype not in _DTYPES or _wide(31, B, T, H, Hk, Dk, Dv, op):
+        return 0
     c = _b.deer_linattn_shape(_DTYPES[dtype], H, Hk, Dk, Dv, 0, 1.0)
     return int(load().deer_linattn_workspace_bytes(ctypes.byref(c), B, T, op))
 
@@ -642,6 +649,8 @@ def _norm(x, w, b, eps):
 
 def deer_layernorm_workspace_bytes(rows: int, G: int, D: int, dtype=torch.float32) -> int:
     """Workspace of deer_layernorm_adjoint; 0 for arguments it refuses."""
+    if dtype not in _DTYPES or _wide(31, G, D) or _wide(63, rows):
+        return 0
     c = _b.deer_norm(_DTYPES[dtype], _b.DEER_F32, G, D, None, None, 0.0)
     return int(load().deer_layernorm_workspace_bytes(ctypes.byref(c), rows))
 
