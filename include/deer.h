@@ -362,7 +362,8 @@ size_t deer_linattn_workspace_bytes(const deer_linattn_shape *shape, int B, int 
  *   log_decay  float32 [H] or [B, T, H] (per_step).  Values are meant to be <= 0; -inf is a
  *              decay of zero: the state starts anew at that step (recordings laid end to end).
  *              Positive values grow the state and are exact as long as the products of the
- *              decays over any 64 steps stay below 2^100 and the states in float32's range.
+ *              decays over any 64 steps stay below 2^100, and the states, the operands times
+ *              such a product and the sums of |q| |S| below 2^127.
  *   lengths    int32 [B] or NULL (T): sequence b has lengths[b] steps (clamped to 0..T).  Rows
  *              at and behind its end are not read; their outputs are zero.
  *   state0     float32 [B, H, Dk, Dv] or NULL (zero): the state before the first step.

@@ -567,7 +567,7 @@ def deer_linattn(q, k, v, log_decay, *, scale: float = 1.0, lengths=None, state0
     S_t = exp(log_decay_t) S_{t-1} + k_t v_t^T, o_t = scale S_t^T q_t.
 
     q, k [B, T, Hk, Dk] and v [B, T, H, Dv] (H a multiple of Hk) in float32, bfloat16 or float16, any
-    strides (views with a unit last stride are read in place); log_decay float32 [H] or [B, T, H];
+    strides (views with a unit last stride are read in place; a step's stride of up to 2^22 elements); log_decay float32 [H] or [B, T, H];
     lengths int32 [B] (steps of each sequence; rows behind them are not read and give zeros);
     state0 float32 [B, H, Dk, Dv].  o and state are buffers for the outputs; state may be state0.
     A NaN or an infinity among the rows that are read may reach any result of its sequence and head.

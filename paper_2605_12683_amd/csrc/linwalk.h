@@ -5,7 +5,8 @@
 //   o_i  = exp(c_i) S^T q_i + sum_{j <= i} exp(c_i - c_j) (k_j q_i) v_j
 //   S   <- exp(L) S + sum_j k_j (exp(L - c_j) v_j)^T.
 // Every exponent is a difference that no decay makes positive, so nothing overflows however small
-// the decays are (factoring exp(c_i) exp(-c_j) would); the sums c are taken in float64 and kept as
+// the decays are (factoring exp(c_i) exp(-c_j) would, and so would leaving the decays of whole chunks out
+// of the state for a while: 24 bits of range for 0 to 1.5% of the time, 1 to 5% where Kd is 256); the sums c are taken in float64 and kept as
 // two floats, so that a difference of two large sums of near size is exact to float32.
 //
 // Products run on the bf16 matrix cores with float32 sums.  Operands of fewer bits enter exactly: a
@@ -327,14 +328,9 @@ struct Decays {
     float hi[C], lo[C];   // log2 decay summed up to each step
     float into[C];        // sc_kv exp2(L - c): what a step's k v^T has left at the chunk's end
     float from[C];        // sc_o exp2(c): what the entering state has left at each step
-    float all;            // factor on the registers that hold the state, at the chunk's end
-    float before, after;  // the state is this times the registers
-    float pad;
+    float all;            // exp2(L): what it has left at the chunk's end
+    float pad[3];
 };
-// The registers hold the state up to a factor 2^ls (the last wave's ls, shared through from, into,
-// before and after), so that the decay of a whole chunk costs no multiplication of every element:
-// it goes into ls, and the registers are only scaled where ls would leave +-kLazy.
-constexpr double kLazy = 24.0;
 
 // the double that the DPP control CTRL brings from another lane, 0 where it brings none
 template <int CTRL, int ROWS>
@@ -345,10 +341,9 @@ __device__ __forceinline__ double dpp_or_zero(double x) {
     return __builtin_bit_cast(double, ((uint64_t)h << 32) | l);
 }
 
-// by one wave; raw: this lane's log decay (C = 32: the upper half wave repeats the lower), ls: of the
-// registers, before and after the chunk.  Returns L.
+// by one wave; raw: this lane's log decay (C = 32: the upper half wave repeats the lower).  Returns L.
 template <int C>
-__device__ __forceinline__ double chunk_decays(Decays<C> &d, float raw, float sc_kv, float sc_o, double &ls) {
+__device__ __forceinline__ double chunk_decays(Decays<C> &d, float raw, float sc_kv, float sc_o) {
     const int lane = threadIdx.x & 63, i = lane & (C - 1);
     double s = gate_of(raw);
     s += dpp_or_zero<0x111, 15>(s);        // row_shr: lanes of each 16
@@ -364,16 +359,9 @@ __device__ __forceinline__ double chunk_decays(Decays<C> &d, float raw, float sc
     const float hi = (float)s;
     d.hi[i] = hi;
     d.lo[i] = (float)(s - (double)hi);
-    d.from[i] = sc_o * __builtin_amdgcn_exp2f((float)(s + ls));
-    const double next = ls + L;
-    const bool lazy = next < kLazy && next > -kLazy;
-    d.into[i] = sc_kv * __builtin_amdgcn_exp2f((float)(lazy ? -(s + ls) : L - s));
-    if (i == 0) {
-        d.before = __builtin_amdgcn_exp2f((float)ls);
-        d.all = lazy ? 1.f : __builtin_amdgcn_exp2f((float)next);
-        d.after = lazy ? __builtin_amdgcn_exp2f((float)next) : 1.f;
-    }
-    ls = lazy ? next : 0.0;
+    d.from[i] = sc_o * __builtin_amdgcn_exp2f(hi);
+    d.into[i] = sc_kv * __builtin_amdgcn_exp2f((float)(L - s));
+    if (i == 0) d.all = __builtin_amdgcn_exp2f((float)L);
     return L;
 }
 
@@ -478,7 +466,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, MODE>
                     add_to(ro.seg_decay[(size_t)bh * a.nseg + s], own + ((long)s - seg) * (long)mat, ro.seg_d, ro.seg_n);
         }
     }
-    auto put_state = [&](float *dst, int sd, int sn, float f) {
+    auto put_state = [&](float *dst, int sd, int sn, float f = 1.f) {
         const auto rsrc = bounded_rsrc(dst, (uint32_t)(mat * 4));
         const int l = afresh((int)threadIdx.x) & 63;
 #pragma unroll
@@ -516,10 +504,10 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, MODE>
         vr.template store<false, false>(Vs, PV);
         if constexpr (OUT) qr.template store<true, false>(Qs, PQ);
     };
-    double total = 0.0, ls = 0.0;                              // last wave: log2 decay of the segment, the registers' scale
+    double total = 0.0;                                        // last wave: log2 decay of the segment
     float raw = 0.f;
     if (w == NW - 1) {
-        const double L = chunk_decays<C>(dec[0], gate(0), ro.sc_kv, ro.sc_o, ls);
+        const double L = chunk_decays<C>(dec[0], gate(0), ro.sc_kv, ro.sc_o);
         if (!OUT) total += L;
         raw = __int_as_float(afresh(__float_as_int(gate(1))));
     }
@@ -542,14 +530,14 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, MODE>
             kr.load(rows_ahead);
             if (!OUT) vr.load(rows_ahead);
             if (w == NW - 1) {
-                const double L = chunk_decays<C>(dec[(n + 1) & 1], next, ro.sc_kv, ro.sc_o, ls);
+                const double L = chunk_decays<C>(dec[(n + 1) & 1], next, ro.sc_kv, ro.sc_o);
                 if (!OUT) total += L;
             }
         }
         float *anc = nullptr;
         if constexpr (DOTS) {
             if (dotted && ((t0 + C) % kLinAnchor == 0 || t0 + C >= a.T)) anc = ro.anchor + ((size_t)bh * na + t0 / kLinAnchor) * mat;
-            if (anc && rev) put_state(anc, N, 1, dc.before);
+            if (anc && rev) put_state(anc, N, 1);
         }
         __builtin_amdgcn_sched_barrier(0);
 
@@ -715,11 +703,10 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, MODE>
         constexpr bool STATE = decltype(state)::value;
         if constexpr (STATE) {
             const float all = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(dc.all)));
-            if (all != 1.f)
 #pragma unroll
-                for (int dt = 0; dt < DT; ++dt)
+            for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-                    for (int ct = 0; ct < CT; ++ct) S[dt][ct] *= all;
+                for (int ct = 0; ct < CT; ++ct) S[dt][ct] *= all;
         }
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
@@ -816,7 +803,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, MODE>
                 dot = group_sum(dot);
                 if (g == 0) dots[w * C + i] = t0 + (rev ? C - 1 - i : i) < len ? dot : 0.f;
             }
-            if (anc && !rev) put_state(anc, N, 1, dc.after);
+            if (anc && !rev) put_state(anc, N, 1);
         }
         lds_barrier();
         if (ahead) {
@@ -886,10 +873,10 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, MODE>
     if constexpr (OUT) {
         if (keep) {
             const float f = rev ? __builtin_amdgcn_exp2f((float)gate_of(gate_raw(a, b, h, -1, len, true))) : 1.f;
-            put_state(ro.fin + bh * mat, ro.fin_d, ro.fin_n, f * dec[(chunks - 1) & 1].after);
+            put_state(ro.fin + bh * mat, ro.fin_d, ro.fin_n, f);
         }
     } else {
-        put_state(ro.seg + ((size_t)bh * a.nseg + seg) * mat, N, 1, dec[(chunks - 1) & 1].after);
+        put_state(ro.seg + ((size_t)bh * a.nseg + seg) * mat, N, 1);
         if (w == NW - 1 && (threadIdx.x & 63) == 0 && tile == 0)
             ro.seg_decay[(size_t)bh * a.nseg + seg] = seg_decay_of(total);
     }

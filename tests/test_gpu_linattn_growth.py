@@ -54,6 +54,24 @@ def test_growth_everywhere(type_, T, monkeypatch):
     check(c, kw, g, monkeypatch)
 
 
+@pytest.mark.parametrize("type_", ["f32", "bf16"])
+@pytest.mark.parametrize("seg", [128, 1 << 20])
+def test_large_states(type_, seg, monkeypatch):
+    """States of up to 2^122 that decay by e^-16 and e^-6 over 64 steps, and products k v as large."""
+    monkeypatch.setenv("DEER_LIN_SEG", str(seg))
+    say("linattn large states", type_, seg)
+    c, kw, g, _ = A.make(1, 300, 2, 1, 8, 40, type_, True, True)
+    c["log_decay"].fill_(-0.25)
+    c["log_decay"][:, :, 1] = -0.1
+    c["k"].clamp_(-1, 1)
+    c["v"].clamp_(-2, 2).mul_(2.0 ** 118)
+    c["q"].clamp_(-2, 2).mul_(2.0 ** -6)
+    g.clamp_(-2, 2).mul_(2.0 ** -6)
+    kw["scale"] = 1.0
+    kw["state0"].clamp_(-2, 2).mul_(2.0 ** 121)
+    check(c, kw, g, monkeypatch)
+
+
 def check(c, kw, g, monkeypatch):
     plain, extra = A.kappa, 2.0 ** -24 * (166 + (32 + 24) * -(-c["v"].shape[1] // 64))
     monkeypatch.setattr(A, "kappa", lambda c, state=False: plain(c, state) + extra)
