@@ -62,13 +62,14 @@ static int seg_override() {
 // Segments: as many as leave all blocks of a walk resident on the chip at once (a few blocks more
 // would run after the others, alone), none of fewer than kMinSeg steps; one where the heads alone give
 // half of that, since segments read k and v a second time.  (2 x 4096 steps, 16 heads of 128 x 128 in
-// bf16, where one segment gives 32 blocks of 512: segments of 256, 512, 1024, 4096 steps take 81, 83,
-// 123, 304 us.)
+// bf16, where one segment gives 32 blocks of 512: segments of 256, 512, 1024, 4096 steps take 85, 87,
+// 102, 241 us.)  An adjoint's are sized for two of its three roles, the third's blocks following as others
+// end (4 x 4096 steps, 16 heads: segments of 512, 1024, 2048 steps 362, 327, 349 us; the rule takes 1024,
+// for three roles it would take 2048).
 constexpr int kMinSeg = 128;
 
 static int segment_steps(const deer_linattn_shape *s, int B, int T, int op) {
     if (const int n = seg_override(); n > 0) return n >= T ? T : (n + 63) / 64 * 64;
-    // the adjoint's walks of dq and dk run together, that of dv by itself
     const bool adj = op == DEER_OP_ADJOINT;
     const int Kd = adj ? s->Dv : s->Dk, N = adj ? s->Dk : s->Dv;
     const long blocks = (long)B * s->H * lin_tiles(Kd, N) * (adj ? 2 : 1);
@@ -80,9 +81,9 @@ static int segment_steps(const deer_linattn_shape *s, int B, int T, int op) {
 }
 
 // Up to this many segments, a walk's block adds up the states before its own segment by itself,
-// beyond that k_lin_join does it once for all (4 x 4096 steps, 16 heads of 128 x 128 in bf16, the
-// adjoint: 4 segments take 336 us, joined 346; 2 x 4096 steps forwards: 8 segments 84, joined 83; 16
-// segments 102, joined 81).
+// beyond that k_lin_join does it once for all (in bf16, 4 segments: 8 x 512 steps of 16 heads of 64 x 64
+// forwards 29.0 us, joined 29.4, the adjoint of 4 x 4096 steps of 16 heads of 128 x 128 327, joined 329;
+// 2 x 4096 steps of those forwards: 8 segments 90, joined 85; 16 segments 101, joined 80).
 constexpr int kMostUnjoined = 4;
 
 static LinArgs args_of(const deer_linattn_shape *s, int B, int T, int op, const float *log_decay,
@@ -268,12 +269,10 @@ int deer_linattn_adjoint(const deer_linattn_shape *s, int B, int T, const deer_v
         ro[1].seg = w.rseg, ro[1].seg_decay = w.rseg_decay;
         ro[1].seg_d = 1, ro[1].seg_n = Dv;                       // R^T: the same states, read across
     }
-    // The walk that leaves dots and anchors takes longer for a chunk; dv has none and runs by itself, but
-    // goes along where all blocks are resident at once (1 x 200 steps, 8 heads of 128 x 128 in bf16: 55 us
-    // apart, 41 together; with more blocks it would wait for theirs: 64 heads of 4096 steps, dq and dk 188
-    // us, dv by itself 94 for 256 of 768 blocks).
-    const bool few = 3L * B * s->H * a.nseg * lin_tiles(Dv, Dk) <= 256L * lin_resident(s->dtype, Dv, Dk, true);
-    if (same && (few || !decay)) {
+    // Where one tile shape serves all three roles they run in one launch, though dv leaves no dots or
+    // anchors (1 x 200 steps, 8 heads of 128 x 128 in bf16: 43 us, dv apart 57; 4 x 4096 steps, 16 heads: 331
+    // and 351; in float32, where blocks of dots are slower, 752 and 728, narrower heads 360 and 377).
+    if (same) {
         if ((rc = launch_lin_walk(a, ro, 3, false, decay, st))) return rc;
     } else if ((rc = launch_lin_walk(a, ro, 2, false, decay, st)) || (rc = launch_lin_walk(a, ro + 2, 1, false, false, st))) {
         return rc;

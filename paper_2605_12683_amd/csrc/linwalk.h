@@ -6,8 +6,9 @@
 //   S   <- exp(L) S + sum_j k_j (exp(L - c_j) v_j)^T.
 // Every exponent is a difference that no decay makes positive, so nothing overflows however small
 // the decays are (factoring exp(c_i) exp(-c_j) would, and so would leaving the decays of whole chunks out
-// of the state for a while: 24 bits of range for 0 to 1.5% of the time, 1 to 5% where Kd is 256); the sums c are taken in float64 and kept as
-// two floats, so that a difference of two large sums of near size is exact to float32.
+// of the state for a while: 24 bits of range for 0 to 1.5% of the time, 1 to 5% where Kd is 256); the
+// sums c are taken in float64 and kept as two floats, so that a difference of two large sums of near
+// size is exact to float32.
 //
 // Products run on the bf16 matrix cores with float32 sums.  Operands of fewer bits enter exactly: a
 // bf16 number as it is, an fp16 number as two bf16 parts, a float32 number as three (split16.h).
@@ -25,12 +26,12 @@
 // transposed by ds_read_b64_tr_b16.  The decayed scores, formed by the four waves tile by tile (those
 // on and below the diagonal), are exchanged through LDS in operand order.
 //
-// What bounds it: a chunk of 64 steps at Kd = N = 128 in bf16 moves 64 KiB and takes 194 matrix
-// instructions of 16 x 16 x 32 a wave (1.5 us at their rate, against 3.3 us for the bytes at 5 TB/s
+// What bounds it: a chunk of 64 steps at Kd = N = 128 in bf16 moves 64 KiB and takes 238 matrix
+// instructions of 16 x 16 x 32 a wave (1.9 us at their rate, against 3.3 us for the bytes at 5 TB/s
 // with all 256 CUs walking).  Between them stand the vector instructions that split and scale what is
-// formed in between: of the issue cycles, vector and matrix instructions fill 58 + 25% (32 heads of
-// 64 x 64, 65536 steps, 768 blocks: 234 us, 2.9 TB/s) or 51 + 33% (dq and dk of 64 heads of 128 x
-// 128, 4096 steps, with dots: 188 us), and LDS is busy for 40%.  So the next chunk's rows are loaded
+// formed in between: of the issue cycles, vector and matrix instructions fill 62 + 29% (32 heads of
+// 64 x 64, 65536 steps, 768 blocks: 250 us, 2.7 TB/s) or 47 + 31% (32 heads of 128 x 128, 4096 steps in
+// segments of 256: 52 us), and LDS is busy for 40% and 22%.  So the next chunk's rows are loaded
 // into registers while this one is computed (barriers order LDS only), the operands of the next
 // products are read from LDS while these run, what depends on the thread alone is not computed again
 // for every row, and tiles are kept below 80 KiB of LDS, C = 32 instead of 64 where needed, so that
@@ -108,9 +109,10 @@ struct LinTile {
     static constexpr bool OUT = MODE != kStates;
     static constexpr int NB = 16 * NW * CT, TH = 64 * NW;
     // LDS row pitches, in which neither rows read 8 or 4 elements a lane nor rows read across meet in
-    // a bank (for 4 elements a lane: with k's columns of each 16 swapped by halves in rows 8..15 of 16);
-    // with KT + 8 for q, k as it is, and the scores' tiles stored apart, 38% of the LDS cycles were
-    // conflicts (32 heads of 64 x 64, 65536 steps: 265 us, 246 without)
+    // a bank (for 4 elements a lane: with k's columns of each 16 swapped by halves in rows 8..15 of 16).
+    // Conflicts still take 14% of the LDS cycles with outputs (32 heads of 64 x 64, 65536 steps) to 21%
+    // (16 heads of 128 x 128), none to 9% without; with KT + 8 for q, k as it is, and the scores' tiles
+    // stored apart, they took 38% and the walk 8% longer.
     static constexpr int PQ = KT + 16, PK = KT + 16, PV = NB + 16;
     static constexpr int pairs(int C) { return C == 64 ? 6 : 2; }   // (16 outputs, 32 sources) not all above the diagonal
     static constexpr int bytes(int C) {
@@ -906,8 +908,8 @@ int launch_walk_tile(const LinArgs &a, const LinRole *roles, int n, hipStream_t 
 template <class Ty, int MODE>
 int launch_walk_mode(const LinArgs &a, const LinRole *roles, int n, hipStream_t st) {
     // Where blocks of 128 columns leave half of the CUs without one, twice as many of 64, which take less
-    // time for a chunk (1 x 2048 steps, 4 heads of 128 x 128 in bf16: 33 us, narrow 27; with up to 256
-    // blocks the second reading of q and k costs more: 64 heads' adjoint 382, narrow 397).  Not with dots,
+    // time for a chunk (1 x 2048 steps, 4 heads of 128 x 128 in bf16: 34 us, narrow 28; with 256 blocks the
+    // second reading of q and k costs more: 8 x 128 steps, 32 heads: 20.6, narrow 22.4).  Not with dots,
     // which are laid out by blocks of 128.
     const int nb = nb_of(kt_of(roles[0].Kd), roles[0].N), tiles = (roles[0].N + nb - 1) / nb;
     const bool narrow = MODE != kOutDots && nb == 128 && (long)a.B * a.H * a.nseg * tiles * n <= 128;
