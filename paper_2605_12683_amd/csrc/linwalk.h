@@ -4,11 +4,10 @@
 // first step to step i (in it), L over the whole chunk and S the state entering it,
 //   o_i  = exp(c_i) S^T q_i + sum_{j <= i} exp(c_i - c_j) (k_j q_i) v_j
 //   S   <- exp(L) S + sum_j k_j (exp(L - c_j) v_j)^T.
-// Every exponent is a difference that no decay makes positive, so nothing overflows however small
-// the decays are (factoring exp(c_i) exp(-c_j) would, and so would leaving the decays of whole chunks out
-// of the state for a while: 24 bits of range for 0 to 1.5% of the time, 1 to 5% where Kd is 256); the
-// sums c are taken in float64 and kept as two floats, so that a difference of two large sums of near
-// size is exact to float32.
+// Every exponent is a difference that no decay makes positive (but for the half that Decays speaks of),
+// so nothing overflows however small the decays are (factoring exp(c_i) exp(-c_j) would); the sums c
+// are taken in float64 and kept as two floats, so that a difference of two large sums of near size is
+// exact to float32.
 //
 // Products run on the bf16 matrix cores with float32 sums.  Operands of fewer bits enter exactly: a
 // bf16 number as it is, an fp16 number as two bf16 parts, a float32 number as three (split16.h).
@@ -328,11 +327,17 @@ __device__ __forceinline__ void mfma_block(const v4u (&x)[X][NA], const v4u (&y)
 template <int C>
 struct Decays {
     float hi[C], lo[C];   // log2 decay summed up to each step
-    float into[C];        // sc_kv exp2(L - c): what a step's k v^T has left at the chunk's end
-    float from[C];        // sc_o exp2(c): what the entering state has left at each step
-    float all;            // exp2(L): what it has left at the chunk's end
-    float pad[3];
+    float into[C];        // sc_kv exp2(L - c - ls'): what a step's k v^T has left at the chunk's end
+    float from[C];        // sc_o exp2(c + ls): what the registers' state has left at each step
+    float all;            // power of two that the registers take at the chunk's end
+    float before, after;  // exp2(ls), exp2(ls'): the state is this times the registers
+    float pad;
 };
+// The registers hold the state up to a factor 2^ls with |ls| <= 1/2, kept in float64 by the last wave.
+// So a chunk's decay multiplies them by a power of two, which rounds nothing: rounded to float32, the
+// same decay in every chunk would be off the same way each time, by 2^-25 for each of the chunks that a
+// state lasts.  (Powers of up to 2^24 left in ls as well would save 0 to 1.5% of the time, 1 to 5% where Kd
+// is 256, and 24 bits of the state's range.)
 
 // the double that the DPP control CTRL brings from another lane, 0 where it brings none
 template <int CTRL, int ROWS>
@@ -343,9 +348,10 @@ __device__ __forceinline__ double dpp_or_zero(double x) {
     return __builtin_bit_cast(double, ((uint64_t)h << 32) | l);
 }
 
-// by one wave; raw: this lane's log decay (C = 32: the upper half wave repeats the lower).  Returns L.
+// by one wave; raw: this lane's log decay (C = 32: the upper half wave repeats the lower), ls: of the
+// registers, before and after the chunk.  Returns L.
 template <int C>
-__device__ __forceinline__ double chunk_decays(Decays<C> &d, float raw, float sc_kv, float sc_o) {
+__device__ __forceinline__ double chunk_decays(Decays<C> &d, float raw, float sc_kv, float sc_o, double &ls) {
     const int lane = threadIdx.x & 63, i = lane & (C - 1);
     double s = gate_of(raw);
     s += dpp_or_zero<0x111, 15>(s);        // row_shr: lanes of each 16
@@ -361,9 +367,15 @@ __device__ __forceinline__ double chunk_decays(Decays<C> &d, float raw, float sc
     const float hi = (float)s;
     d.hi[i] = hi;
     d.lo[i] = (float)(s - (double)hi);
-    d.from[i] = sc_o * __builtin_amdgcn_exp2f(hi);
-    d.into[i] = sc_kv * __builtin_amdgcn_exp2f((float)(L - s));
-    if (i == 0) d.all = __builtin_amdgcn_exp2f((float)L);
+    d.from[i] = sc_o * __builtin_amdgcn_exp2f((float)(s + ls));
+    const double next = ls + L, whole = __builtin_rint(next);
+    d.into[i] = sc_kv * __builtin_amdgcn_exp2f((float)(whole - (s + ls)));
+    if (i == 0) {
+        d.before = __builtin_amdgcn_exp2f((float)ls);
+        d.all = __builtin_amdgcn_ldexpf(1.f, (int)whole);
+        d.after = __builtin_amdgcn_exp2f((float)(next - whole));
+    }
+    ls = next - whole;
     return L;
 }
 
@@ -468,7 +480,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, MODE>
                     add_to(ro.seg_decay[(size_t)bh * a.nseg + s], own + ((long)s - seg) * (long)mat, ro.seg_d, ro.seg_n);
         }
     }
-    auto put_state = [&](float *dst, int sd, int sn, float f = 1.f) {
+    auto put_state = [&](float *dst, int sd, int sn, float f) {
         const auto rsrc = bounded_rsrc(dst, (uint32_t)(mat * 4));
         const int l = afresh((int)threadIdx.x) & 63;
 #pragma unroll
@@ -506,10 +518,10 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, MODE>
         vr.template store<false, false>(Vs, PV);
         if constexpr (OUT) qr.template store<true, false>(Qs, PQ);
     };
-    double total = 0.0;                                        // last wave: log2 decay of the segment
+    double total = 0.0, ls = 0.0;                              // last wave: log2 decay of the segment, the registers' scale
     float raw = 0.f;
     if (w == NW - 1) {
-        const double L = chunk_decays<C>(dec[0], gate(0), ro.sc_kv, ro.sc_o);
+        const double L = chunk_decays<C>(dec[0], gate(0), ro.sc_kv, ro.sc_o, ls);
         if (!OUT) total += L;
         raw = __int_as_float(afresh(__float_as_int(gate(1))));
     }
@@ -532,14 +544,14 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, MODE>
             kr.load(rows_ahead);
             if (!OUT) vr.load(rows_ahead);
             if (w == NW - 1) {
-                const double L = chunk_decays<C>(dec[(n + 1) & 1], next, ro.sc_kv, ro.sc_o);
+                const double L = chunk_decays<C>(dec[(n + 1) & 1], next, ro.sc_kv, ro.sc_o, ls);
                 if (!OUT) total += L;
             }
         }
         float *anc = nullptr;
         if constexpr (DOTS) {
             if (dotted && ((t0 + C) % kLinAnchor == 0 || t0 + C >= a.T)) anc = ro.anchor + ((size_t)bh * na + t0 / kLinAnchor) * mat;
-            if (anc && rev) put_state(anc, N, 1);
+            if (anc && rev) put_state(anc, N, 1, dc.before);
         }
         __builtin_amdgcn_sched_barrier(0);
 
@@ -705,10 +717,11 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, MODE>
         constexpr bool STATE = decltype(state)::value;
         if constexpr (STATE) {
             const float all = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(dc.all)));
+            if (all != 1.f)
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
+                for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-                for (int ct = 0; ct < CT; ++ct) S[dt][ct] *= all;
+                    for (int ct = 0; ct < CT; ++ct) S[dt][ct] *= all;
         }
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
@@ -805,7 +818,7 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, MODE>
                 dot = group_sum(dot);
                 if (g == 0) dots[w * C + i] = t0 + (rev ? C - 1 - i : i) < len ? dot : 0.f;
             }
-            if (anc && !rev) put_state(anc, N, 1);
+            if (anc && !rev) put_state(anc, N, 1, dc.after);
         }
         lds_barrier();
         if (ahead) {
@@ -875,10 +888,10 @@ __global__ __launch_bounds__(64 * NW, (LinTile<InParts<Ty>::n, KT, NW, CT, MODE>
     if constexpr (OUT) {
         if (keep) {
             const float f = rev ? __builtin_amdgcn_exp2f((float)gate_of(gate_raw(a, b, h, -1, len, true))) : 1.f;
-            put_state(ro.fin + bh * mat, ro.fin_d, ro.fin_n, f);
+            put_state(ro.fin + bh * mat, ro.fin_d, ro.fin_n, f * dec[(chunks - 1) & 1].after);
         }
     } else {
-        put_state(ro.seg + ((size_t)bh * a.nseg + seg) * mat, N, 1);
+        put_state(ro.seg + ((size_t)bh * a.nseg + seg) * mat, N, 1, dec[(chunks - 1) & 1].after);
         if (w == NW - 1 && (threadIdx.x & 63) == 0 && tile == 0)
             ro.seg_decay[(size_t)bh * a.nseg + seg] = seg_decay_of(total);
     }

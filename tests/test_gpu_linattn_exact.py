@@ -106,3 +106,28 @@ def test_whole_products(type_, top, B, H):
         for name, a, want in (("o", r["o"], o), ("state", r["state"], last), *((n, got[n], ref[n]) for n in "qkv"),
                               ("log_decay", got["log_decay"], ref["log_decay"])):
             same(name, a, torch.tensor(want).float().to(a.dtype).cuda())
+
+
+@pytest.mark.parametrize("seg", [1 << 20, 25024])     # one segment, or eight
+@pytest.mark.parametrize("per_step", [False, True])
+def test_slow_decays(seg, per_step, monkeypatch):
+    """200000 steps that only decay, by e^-5 and e^-0.3 in all: what is left is off by the few roundings at
+    the segments' ends, not by one for each of 3125 chunks of steps (2^-25 a chunk, the same way each time,
+    would be 1500 half steps). A half step is 2^-24. At each of n segments' ends: the decay's factor (two,
+    of a hardware exponential, and one of its exponent), the sum; at the last: the power of two, its
+    exponent, a product, and the step that the adjoint adds (four)."""
+    monkeypatch.setenv("DEER_LIN_SEG", str(seg))
+    say("linattn slow decays", seg, per_step)
+    B, T, H, Dk, Dv = 1, 200000, 2, 8, 8
+    rng = np.random.default_rng(3)
+    ld = np.array([-2.5e-5, -1.5e-6], np.float32)
+    s0, gs = (torch.tensor(rng.standard_normal((B, H, Dk, Dv))).float().cuda() for _ in range(2))
+    zero = torch.zeros(B, T, H, Dk, device="cuda")
+    dec = torch.tensor(ld).cuda()
+    args = (zero, zero, zero, dec.expand(B, T, H) if per_step else dec)
+    left = torch.tensor(np.exp(ld.astype(np.float64) * T)).cuda()[:, None, None]
+    tol = 2.0 ** -24 * (4 * -(-T // seg) + 8)
+    state = D.deer_linattn(*args, state0=s0, want_state=True)["state"]
+    assert ((state.double() / (s0.double() * left) - 1).abs() <= tol).all()
+    back = D.deer_linattn_adjoint(*args, zero, state0=s0, g_state=gs)["grads"]["state0"]
+    assert ((back.double() / (gs.double() * left) - 1).abs() <= tol).all()
