@@ -29,7 +29,7 @@
 // instructions of 16 x 16 x 32 a wave (1.9 us at their rate, against 3.3 us for the bytes at 5 TB/s
 // with all 256 CUs walking).  Between them stand the vector instructions that split and scale what is
 // formed in between: of the issue cycles, vector and matrix instructions fill 62 + 29% (32 heads of
-// 64 x 64, 65536 steps, 768 blocks: 250 us, 2.7 TB/s) or 47 + 31% (32 heads of 128 x 128, 4096 steps in
+// 64 x 64, 65536 steps, 768 blocks: 250 us, 2.7 TB/s) or 46 + 30% (32 heads of 128 x 128, 4096 steps in
 // segments of 256: 52 us), and LDS is busy for 40% and 22%.  So the next chunk's rows are loaded
 // into registers while this one is computed (barriers order LDS only), the operands of the next
 // products are read from LDS while these run, what depends on the thread alone is not computed again
@@ -109,8 +109,8 @@ struct LinTile {
     static constexpr int NB = 16 * NW * CT, TH = 64 * NW;
     // LDS row pitches, in which neither rows read 8 or 4 elements a lane nor rows read across meet in
     // a bank (for 4 elements a lane: with k's columns of each 16 swapped by halves in rows 8..15 of 16).
-    // Conflicts still take 14% of the LDS cycles with outputs (32 heads of 64 x 64, 65536 steps) to 21%
-    // (16 heads of 128 x 128), none to 9% without; with KT + 8 for q, k as it is, and the scores' tiles
+    // Conflicts still take 9 to 21% of the LDS cycles of walks with outputs (14% with 32 heads of 64 x 64,
+    // 65536 steps, 21% with heads of 128 x 128) and none to 9% of those without; with KT + 8 for q, k as it is, and the scores' tiles
     // stored apart, they took 38% and the walk 8% longer.
     static constexpr int PQ = KT + 16, PK = KT + 16, PV = NB + 16;
     static constexpr int pairs(int C) { return C == 64 ? 6 : 2; }   // (16 outputs, 32 sources) not all above the diagonal
@@ -336,8 +336,8 @@ struct Decays {
 // The registers hold the state up to a factor 2^ls with |ls| <= 1/2, kept in float64 by the last wave.
 // So a chunk's decay multiplies them by a power of two, which rounds nothing: rounded to float32, the
 // same decay in every chunk would be off the same way each time, by 2^-25 for each of the chunks that a
-// state lasts.  (Powers of up to 2^24 left in ls as well would save 0 to 1.5% of the time, 1 to 5% where Kd
-// is 256, and 24 bits of the state's range.)
+// state lasts.  (Leaving powers of up to 2^24 in ls as well would save 0 to 4% of the time and cost 24
+// bits of the state's range.)
 
 // the double that the DPP control CTRL brings from another lane, 0 where it brings none
 template <int CTRL, int ROWS>
